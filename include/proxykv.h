@@ -52,12 +52,13 @@ typedef enum {
   PROXYKV_EINVAL = -1,       /* null pointer, non-positive size, ratio outside (0,1], K outside [1,N], ... */
   PROXYKV_EUNSUPPORTED = -2, /* a shape or switch this build has no kernel for */
   PROXYKV_ENOMEM = -3,       /* device allocation failed */
-  PROXYKV_ESTATE = -4,       /* mapper weights not set, context destroyed, ... */
+  PROXYKV_ESTATE = -4,       /* mapper weights not set, workspace to be allocated while the stream captures, ... */
   PROXYKV_EHIP = -5,         /* a HIP runtime call failed */
   PROXYKV_ELIMIT = -6        /* a size beyond the fixed limit that the entry point documents */
 } proxykv_status;
 
-typedef enum { PROXYKV_BF16 = 0, PROXYKV_FP32 = 1 } proxykv_dtype;
+/* FP16 is for the target's cache (proxykv_attend, proxykv_attend_shared); the proxy's queries and keys are bf16 or fp32. */
+typedef enum { PROXYKV_BF16 = 0, PROXYKV_FP32 = 1, PROXYKV_FP16 = 2 } proxykv_dtype;
 
 /* Reduction over the query axis that turns attention probabilities into a per-key score.
  * MAX: maximum over reconstruction queries and over the query heads of a GQA group (the
@@ -229,6 +230,59 @@ int proxykv_topk_pooled(proxykv_ctx* ctx, const float* scores, int64_t layers, i
 int proxykv_compact_pooled(proxykv_ctx* ctx, void* k, void* v, const int32_t* flat,
                            const int32_t* counts, int64_t layers, int64_t heads, int64_t N, int64_t K,
                            int64_t D, void* stream);
+
+/* Attention of a layer's new tokens over its compacted cache (Sec. 4.3: decode runs on the target alone, on what the mask has kept).
+ *   q [rows, group, T, D]  the T newest tokens' queries (post-RoPE) of the `group` query heads of every row, a row being a (sequence,
+ *                          KV head): [batch, H_q, T, D] as it lies, with rows = batch * H_kv
+ *   k, v [rows, N, D]      the cache, with room for N tokens a row; the T new tokens' own keys and values are in it, as the row's last
+ *   lens [rows] int32      tokens of every row (what proxykv_topk_pooled counts, what proxykv_evict leaves, plus what was appended since);
+ *                          NULL: N each.  Values outside [0, N] count as the nearest of the two.
+ *   dtype                  PROXYKV_BF16 or PROXYKV_FP16, of q, k, v and out
+ *   out [rows, group, T, D]
+ *   weight [rows, N] fp32  an account of attention, or NULL: see below
+ * New token t sees the row's tokens n < lens - T + 1 + t; probabilities are the softmax of <q, k> / sqrt(D) over them, and out their sum
+ * of v.  A query that sees nothing (an empty row, or more new tokens than the row has) gets zeros.  Whatever lies in k, v and
+ * weight behind a row's tokens is not used, and weight there is left as it was; a token that only some of the T queries see does not touch
+ * the others, NaN and infinities in it included.
+ * weight[r, n] += the sum of the probabilities that token n gets from the row's group * T queries: over a decode, how much of the
+ * attention every cached token has had, by which proxykv_evict selects.  The caller clears it for new tokens.
+ * Products of q and k run on MFMA with fp32 accumulation, softmax in fp32; for the product with v a probability is split into
+ * two 16-bit values.  Results do not depend on what else runs: no sum is taken in an order that varies.
+ * D in {64, 128} (PROXYKV_EUNSUPPORTED otherwise), T <= N, rows * group * T < 2^23; weight and lens may lie on any 4-byte boundary.
+ * While the stream captures, the call allocates nothing and returns PROXYKV_ESTATE if the context has not served one as large
+ * (in each of rows, group * T and N) before: make the largest call once before capturing. */
+int proxykv_attend(proxykv_ctx* ctx, const void* q, const void* k, const void* v, const int32_t* lens,
+                   int32_t dtype, int64_t rows, int64_t N, int64_t group, int64_t T, int64_t D, void* out,
+                   float* weight, void* stream);
+
+/* The same for a batch of sequences that share a long compacted context, which is read once for all of them:
+ *   q [batch, heads, group, T, D]; k_shared, v_shared [heads, P, D] with shared_lens [heads] tokens (NULL: P each); k, v
+ *   [batch, heads, N, D] the sequences' own tokens with lens [batch, heads] (NULL: N each); out [batch, heads, group, T, D].
+ * New token t of a sequence sees all shared tokens and its own n < lens - T + 1 + t, in one softmax.  Every sequence's new tokens are the
+ * last of its own; N = 0 (then k, v and lens are not used): there are no own tokens, and the queries see the shared ones.
+ *   weight_shared [heads, P] fp32: += what the shared tokens get from all sequences; weight [batch, heads, N] as in proxykv_attend; each
+ *   may be NULL.
+ * Types, limits and everything else as proxykv_attend, with rows = batch * heads. */
+int proxykv_attend_shared(proxykv_ctx* ctx, const void* q, const void* k_shared, const void* v_shared,
+                          const int32_t* shared_lens, const void* k, const void* v, const int32_t* lens,
+                          int32_t dtype, int64_t batch, int64_t heads, int64_t P, int64_t N, int64_t group,
+                          int64_t T, int64_t D, void* out, float* weight_shared, float* weight, void* stream);
+
+/* Eviction by accumulated attention weight, for a cache that has grown past its budget while it was decoded on: k, v [rows, N, D] 16-bit
+ * elements, weight [rows, N] fp32 (proxykv_attend's account), positions [rows, N] int32 (anything that goes with a token, such as its
+ * place in the text; may be NULL) and lens [rows] int32 are changed where they lie.
+ * A row of n = lens[r] tokens with a budget of b < n keeps its last `recent` tokens and the keep = b - recent heaviest of the n - recent
+ * candidates in front of them (equal weights: the lower slot; -0.0 == +0.0; NaN below every number).  A kept candidate in one of the first
+ * `keep` slots stays there; the kept ones behind them move, first to first, into the slots that were given up; the recent tokens follow
+ * in slots keep .. b - 1, in order (the keys hold their rotary positions, so the order of the others means nothing to attention, and few
+ * tokens move).  lens[r] becomes b; what lies behind is left as it was.  Rows of no more than b tokens are not touched.
+ *   budgets [rows] int32 (DEVICE): a budget for every row, such as proxykv_topk_pooled's counts, and `budget` is not used; values outside
+ *   [recent, N] count as the nearest of the two.  NULL: `budget` for all, 1 <= budget <= N, recent <= budget.
+ * 0 <= recent <= N; D*2 bytes a multiple of 16 and at most 512; rows < 2^21.  The workspace (4 bytes * rows * N) and captured calls are as
+ * with proxykv_attend. */
+int proxykv_evict(proxykv_ctx* ctx, void* k, void* v, float* weight, int32_t* positions, int32_t* lens,
+                  const int32_t* budgets, int64_t rows, int64_t N, int64_t budget, int64_t recent, int64_t D,
+                  void* stream);
 
 /* The whole path on one stream: score -> map -> top-k -> compact, with
  * K = proxykv_keep_count(N, keep_ratio) written to *K_host (HOST, may be NULL).

@@ -28,5 +28,7 @@ from .proxykv_oracle import (  # noqa: F401
     topk_pooled,
     mask,
     compact,
+    attend,
+    evict,
     prune,
 )

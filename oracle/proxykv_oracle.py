@@ -500,6 +500,69 @@ def compact(kv: torch.Tensor, idx: torch.Tensor) -> torch.Tensor:
     return torch.gather(kv, -2, gather_index)
 
 
+# --------------------------------------------------------------------------
+# Decoding on the compacted cache
+# --------------------------------------------------------------------------
+
+def attend(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, lens: Optional[Sequence[int]] = None,
+           k_shared: Optional[torch.Tensor] = None, v_shared: Optional[torch.Tensor] = None,
+           shared_lens: Optional[Sequence[int]] = None):
+    """Attention of the T newest tokens over a cache of rows of their own lengths (Sec. 4.3: decode runs
+    on what the mask has kept).  q [B, H, G, T, D], k and v [B, H, N, D], lens [B][H]; the T new tokens are
+    the last of a row, and token t sees n < lens - T + 1 + t, besides all shared tokens (k_shared, v_shared
+    [H, P, D], shared_lens [H]) if there are any.  Returns (out [B, H, G, T, D], weight [B, H, N], weight_shared
+    [H, P] or None, spread [B, H, G, T, D]): the softmax-weighted sum of v, what every token gets in
+    probability, and the same sum of |v|.  A query that sees nothing has zeros."""
+    B, H, G, T, D = q.shape
+    N = k.shape[2]
+    P = 0 if k_shared is None else k_shared.shape[1]
+    out = torch.zeros(B, H, G, T, D, dtype=F64)
+    spread = torch.zeros_like(out)
+    weight = torch.zeros(B, H, N, dtype=F64)
+    weight_shared = torch.zeros(H, P, dtype=F64) if P else None
+    for b in range(B):
+        for h in range(H):
+            n = N if lens is None else min(max(int(lens[b][h]), 0), N)
+            p_len = 0 if not P else P if shared_lens is None else min(max(int(shared_lens[h]), 0), P)
+            for t in range(T):
+                m = max(n - T + 1 + t, 0)
+                keys, vals = k[b, h, :m].to(F64), v[b, h, :m].to(F64)
+                if p_len:
+                    keys, vals = torch.cat([k_shared[h, :p_len].to(F64), keys]), torch.cat([v_shared[h, :p_len].to(F64), vals])
+                if keys.shape[0] == 0:
+                    continue
+                p = torch.softmax(q[b, h, :, t].to(F64) @ keys.T / math.sqrt(D), dim=-1)
+                out[b, h, :, t], spread[b, h, :, t] = p @ vals, p @ vals.abs()
+                weight[b, h, :m] += p[:, p_len:].sum(0)
+                if p_len:
+                    weight_shared[h, :p_len] += p[:, :p_len].sum(0)
+    return out, weight, weight_shared, spread
+
+
+def evict(weight: torch.Tensor, lens: Sequence[int], budgets: Sequence[int], recent: int):
+    """Eviction by accumulated attention weight, as an index: source [rows, N] with new[r, j] = old[r, source[r, j]]
+    for everything that goes with a token, and the new lengths.  A row of n > b tokens keeps its `recent` last and the
+    b - recent heaviest of the others (ties to the lower slot, NaN below every number).  Kept tokens among the first
+    b - recent slots stay, those behind fill the free slots in order, the recent ones follow in order."""
+    rows, N = weight.shape
+    source = torch.arange(N).repeat(rows, 1)
+    new_lens = []
+    for r in range(rows):
+        n, b = min(max(int(lens[r]), 0), N), min(max(int(budgets[r]), recent), N)
+        if n <= b:
+            new_lens.append(int(lens[r]))
+            continue
+        new_lens.append(b)
+        cand, keep = n - recent, b - recent
+        kept = topk(weight[r:r + 1, :cand], keep)[0].tolist() if keep else []
+        behind = [i for i in kept if i >= keep]
+        free = sorted(set(range(keep)) - set(kept))
+        for i, j in zip(behind, free):
+            source[r, j] = i
+        source[r, keep:b] = torch.arange(cand, n)
+    return source, new_lens
+
+
 def prune(q_rec: torch.Tensor, k_ctx: torch.Tensor, k_rec: torch.Tensor, chunk: int, keep_ratio: float,
           w: Weights, k_t: torch.Tensor, v_t: torch.Tensor, n_heads: int = 8, win: int = 2048,
           stride: int = 1024):

@@ -14,7 +14,7 @@ _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libproxykv.so")
 
 PROXYKV_OK, PROXYKV_EINVAL, PROXYKV_EUNSUPPORTED, PROXYKV_ENOMEM, PROXYKV_ESTATE, PROXYKV_EHIP, PROXYKV_ELIMIT = 0, -1, -2, -3, -4, -5, -6
-PROXYKV_BF16, PROXYKV_FP32 = 0, 1
+PROXYKV_BF16, PROXYKV_FP32, PROXYKV_FP16 = 0, 1, 2
 PROXYKV_REDUCE_MAX, PROXYKV_REDUCE_SUM = 0, 1
 
 EXPORTS = [
@@ -22,7 +22,8 @@ EXPORTS = [
     "proxykv_set_mapper_weights", "proxykv_workspace_bytes", "proxykv_reserve", "proxykv_keep_count",
     "proxykv_layer_pairing", "proxykv_score", "proxykv_score_self", "proxykv_map", "proxykv_topk", "proxykv_topk_static",
     "proxykv_topk_static_limit", "proxykv_compact", "proxykv_compact_inplace",
-    "proxykv_mask", "proxykv_topk_pooled", "proxykv_compact_pooled", "proxykv_prune", "proxykv_set_fused_select",
+    "proxykv_mask", "proxykv_topk_pooled", "proxykv_compact_pooled", "proxykv_attend", "proxykv_attend_shared",
+    "proxykv_evict", "proxykv_prune", "proxykv_set_fused_select",
     "proxykv_profile_enable", "proxykv_profile_read", "proxykv_strerror", "proxykv_last_hip_error",
 ]
 STAGES = ("score_lse", "score_colmax", "map", "topk", "compact")
@@ -77,6 +78,9 @@ def load() -> ctypes.CDLL:
     lib.proxykv_mask.argtypes = [vp, vp, i64, i64, i64, vp, vp]
     lib.proxykv_topk_pooled.argtypes = [vp, vp, i64, i64, i64, i64, vp, vp, vp]
     lib.proxykv_compact_pooled.argtypes = [vp, vp, vp, vp, vp, i64, i64, i64, i64, i64, vp]
+    lib.proxykv_attend.argtypes = [vp, vp, vp, vp, vp, i32, i64, i64, i64, i64, i64, vp, vp, vp]
+    lib.proxykv_attend_shared.argtypes = [vp, vp, vp, vp, vp, vp, vp, vp, i32, i64, i64, i64, i64, i64, i64, i64, vp, vp, vp, vp]
+    lib.proxykv_evict.argtypes = [vp, vp, vp, vp, vp, vp, vp, i64, i64, i64, i64, i64, vp]
     lib.proxykv_prune.argtypes = [vp, vp, vp, vp, i32, i64, i64, i32, f64, vp, vp, vp, vp, vp, vp, vp,
                                   ctypes.POINTER(i64), vp]
     lib.proxykv_set_fused_select.argtypes = [vp, ctypes.c_int]
@@ -228,6 +232,11 @@ def _stream_ptr(stream) -> Optional[int]:
     return stream.cuda_stream or None
 
 
+def _stream_on(ctx: Context, stream) -> Optional[int]:
+    """The stream's handle; without one, that of the current stream of the context's device, whatever the current device is."""
+    return _stream_ptr(torch.cuda.current_stream(ctx.cfg.device) if stream is None else stream)
+
+
 def _qk_dtype(q: torch.Tensor) -> int:
     if q.dtype == torch.bfloat16:
         return PROXYKV_BF16
@@ -351,6 +360,95 @@ def proxykv_compact_pooled(ctx: Context, k, v, flat, counts, stream=None) -> Non
     _check(load().proxykv_compact_pooled(ctx.handle, _dev_ptr(k, "k"), _dev_ptr(v, "v"), _dev_ptr(flat, "flat", torch.int32),
                                          _dev_ptr(counts, "counts", torch.int32), layers, heads, N, K, D, _stream_ptr(stream)),
            "proxykv_compact_pooled", ctx.handle)
+
+
+def _on_device(ctx: Context, **tensors) -> None:
+    for name, t in tensors.items():
+        if t is not None and (not t.is_cuda or t.device.index != ctx.cfg.device):
+            raise ValueError(f"{name} must be on the context's device cuda:{ctx.cfg.device}, not {t.device}")
+
+
+def _expect(name: str, t: Optional[torch.Tensor], shape, dtype) -> None:
+    if t is not None and (tuple(t.shape) != tuple(shape) or t.dtype != dtype):
+        raise ValueError(f"{name} must be {dtype} {tuple(shape)}, got {t.dtype} {tuple(t.shape)}")
+
+
+def _cache_dtype(q: torch.Tensor) -> int:
+    if q.dtype == torch.bfloat16:
+        return PROXYKV_BF16
+    if q.dtype == torch.float16:
+        return PROXYKV_FP16
+    raise ValueError("the cache and its queries must be bf16 or fp16")
+
+
+def proxykv_attend(ctx: Context, q, k, v, lens=None, weight=None, out=None, stream=None) -> torch.Tensor:
+    """Attention of new tokens over a layer's cache: q [..., group, T, D], k and v [..., N, D], lens int32 [...] tokens per row (None: N);
+    weight fp32 [..., N], if given, is added every token's probabilities.  The leading dimensions are the rows."""
+    (group, T, D), N, rows = q.shape[-3:], k.shape[-2], q.shape[:-3]
+    _on_device(ctx, q=q, k=k, v=v, lens=lens, weight=weight, out=out)
+    _expect("k", k, (*rows, N, D), q.dtype)
+    _expect("v", v, (*rows, N, D), q.dtype)
+    _expect("lens", lens, rows, torch.int32)
+    _expect("weight", weight, (*rows, N), torch.float32)
+    _expect("out", out, q.shape, q.dtype)
+    if out is None:
+        out = torch.empty_like(q, memory_format=torch.contiguous_format)
+    _check(load().proxykv_attend(ctx.handle, _dev_ptr(q, "q"), _dev_ptr(k, "k"), _dev_ptr(v, "v"), _dev_ptr(lens, "lens"), _cache_dtype(q),
+                                 rows.numel(), N, group, T, D, _dev_ptr(out, "out"), _dev_ptr(weight, "weight"), _stream_on(ctx, stream)),
+           "proxykv_attend", ctx.handle)
+    return out
+
+
+def proxykv_attend_shared(ctx: Context, q, k_shared, v_shared, k=None, v=None, shared_lens=None, lens=None, weight_shared=None, weight=None,
+                          out=None, stream=None) -> torch.Tensor:
+    """The same for a batch that shares a long context: q [batch, heads, group, T, D], k_shared and v_shared [heads, P, D] with shared_lens
+    int32 [heads], k and v [batch, heads, N, D] (None: no tokens of their own) with lens int32 [batch, heads]; weight_shared fp32 [heads, P] and
+    weight fp32 [batch, heads, N], if given, are added every token's probabilities."""
+    batch, heads, group, T, D = q.shape
+    P = k_shared.shape[-2]
+    if (k is None) != (v is None):
+        raise ValueError("k and v go together")
+    if k is None and not (lens is None and weight is None):
+        raise ValueError("lens and weight are those of own tokens, k and v")
+    N = 0 if k is None else k.shape[-2]
+    _on_device(ctx, q=q, k_shared=k_shared, v_shared=v_shared, k=k, v=v, shared_lens=shared_lens, lens=lens, weight_shared=weight_shared,
+               weight=weight, out=out)
+    for name, t in (("k_shared", k_shared), ("v_shared", v_shared)):
+        _expect(name, t, (heads, P, D), q.dtype)
+    for name, t in (("k", k), ("v", v)):
+        _expect(name, t, (batch, heads, N, D), q.dtype)
+    _expect("shared_lens", shared_lens, (heads,), torch.int32)
+    _expect("lens", lens, (batch, heads), torch.int32)
+    _expect("weight_shared", weight_shared, (heads, P), torch.float32)
+    _expect("weight", weight, (batch, heads, N), torch.float32)
+    _expect("out", out, q.shape, q.dtype)
+    if out is None:
+        out = torch.empty_like(q, memory_format=torch.contiguous_format)
+    own = N > 0
+    _check(load().proxykv_attend_shared(ctx.handle, _dev_ptr(q, "q"), _dev_ptr(k_shared, "k_shared"), _dev_ptr(v_shared, "v_shared"),
+                                        _dev_ptr(shared_lens, "shared_lens"), _dev_ptr(k, "k") if own else None, _dev_ptr(v, "v") if own else None,
+                                        _dev_ptr(lens, "lens"), _cache_dtype(q), batch, heads, P, N, group, T, D, _dev_ptr(out, "out"),
+                                        _dev_ptr(weight_shared, "weight_shared"), _dev_ptr(weight, "weight") if own else None,
+                                        _stream_on(ctx, stream)), "proxykv_attend_shared", ctx.handle)
+    return out
+
+
+def proxykv_evict(ctx: Context, k, v, weight, lens, budget, recent: int, positions=None, stream=None) -> None:
+    """Rows of k, v [..., N, D], weight fp32 [..., N], positions int32 [..., N] (or None) and lens int32 [...] that hold more than `budget` tokens
+    are cut to it where they lie: the `recent` last tokens and the heaviest others stay.  budget: an int, or an int32 tensor [...]."""
+    N, D, rows = k.shape[-2], k.shape[-1], k.shape[:-2]
+    budgets = budget if isinstance(budget, torch.Tensor) else None
+    _on_device(ctx, k=k, v=v, weight=weight, lens=lens, positions=positions, budget=budgets)
+    if k.element_size() != 2:
+        raise ValueError("k and v must have 16-bit elements")
+    _expect("v", v, k.shape, k.dtype)
+    _expect("weight", weight, (*rows, N), torch.float32)
+    _expect("lens", lens, rows, torch.int32)
+    _expect("positions", positions, (*rows, N), torch.int32)
+    _expect("budget", budgets, rows, torch.int32)
+    _check(load().proxykv_evict(ctx.handle, _dev_ptr(k, "k"), _dev_ptr(v, "v"), _dev_ptr(weight, "weight"), _dev_ptr(positions, "positions"),
+                                _dev_ptr(lens, "lens"), _dev_ptr(budgets, "budget"), rows.numel(), N, 0 if budgets is not None else int(budget),
+                                recent, D, _stream_on(ctx, stream)), "proxykv_evict", ctx.handle)
 
 
 def proxykv_prune(ctx: Context, q_rec, k_ctx, k_rec, chunk: int, keep_ratio: float, k_in, v_in, k_out=None, v_out=None,

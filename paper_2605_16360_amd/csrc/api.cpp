@@ -4,6 +4,7 @@
 #include <string.h>
 
 #include <algorithm>
+#include <initializer_list>
 #include <new>
 #include <vector>
 
@@ -42,6 +43,8 @@ int validate_config(const proxykv_config* c) {
     return PROXYKV_EUNSUPPORTED;
   return PROXYKV_OK;
 }
+
+constexpr int64_t kAttendQueryUnit = 256;  // work-items of a launch per query: a launch counts them in 32 bits
 
 int validate_lengths(int64_t N, int64_t N_q, int64_t chunk) {
   if (N <= 0 || N_q <= 0 || chunk <= 0) return PROXYKV_EINVAL;
@@ -428,6 +431,37 @@ int score_self_impl(proxykv_ctx* ctx, const void* q_in, const void* k_in, int32_
   return PROXYKV_OK;
 }
 
+// Workspace of a call that may be under capture, where nothing can be allocated: then what is there has to do
+int ensure_captured(proxykv_ctx* ctx, DeviceBuffer& b, size_t bytes, hipStream_t stream) {
+  if (bytes > b.bytes && capturing(stream)) return PROXYKV_ESTATE;
+  return ensure(ctx, b, bytes, stream);
+}
+
+inline bool aligned(const void* p, size_t n) { return ((uintptr_t)p & (n - 1)) == 0; }
+
+// What proxykv_attend (no shared tokens) and proxykv_attend_shared have in common
+int attend_impl(proxykv_ctx* ctx, const pkv::AttendArgs& a, int32_t dtype, hipStream_t stream) {
+  if (!aligned(a.q, 16) || !aligned(a.k, 16) || !aligned(a.v, 16) || !aligned(a.k_shared, 16) || !aligned(a.v_shared, 16) || !aligned(a.out, 16) ||
+      !aligned(a.lens, 4) || !aligned(a.shared_lens, 4) || !aligned(a.weight, 4) || !aligned(a.weight_shared, 4))
+    return PROXYKV_EINVAL;
+  if (dtype != PROXYKV_BF16 && dtype != PROXYKV_FP16) return dtype == PROXYKV_FP32 ? PROXYKV_EUNSUPPORTED : PROXYKV_EINVAL;
+  if (a.D != 64 && a.D != 128) return PROXYKV_EUNSUPPORTED;
+  PKV_HIP(ctx, hipSetDevice(ctx->cfg.device));
+  const int rc = ensure_captured(ctx, ctx->attend_ws, pkv::attend_scratch_bytes(a), stream);
+  if (rc) return rc;
+  PKV_HIP(ctx, pkv::launch_attend(a, ctx->attend_ws.ptr, stream));
+  return PROXYKV_OK;
+}
+// factors >= 1 whose product stays below 2^31
+bool product_fits(std::initializer_list<int64_t> factors) {
+  int64_t n = 1;
+  for (int64_t f : factors) {
+    if (f <= 0 || f >= (1ll << 31) / n) return false;
+    n *= f;
+  }
+  return true;
+}
+
 int map_impl(proxykv_ctx* ctx, const float* x, int64_t N, float* yhat, hipStream_t stream) {
   int rc;
   pkv::MapPlan p;
@@ -473,7 +507,8 @@ int proxykv_create(proxykv_ctx** out, const proxykv_config* cfg) {
 int proxykv_destroy(proxykv_ctx* ctx) {
   if (!ctx) return PROXYKV_OK;
   std::vector<DeviceBuffer*> all = {&ctx->weight_blob, &ctx->block_blob, &ctx->q_bf16, &ctx->kctx_bf16, &ctx->krec_bf16,
-                                    &ctx->neg_lse, &ctx->x_parts, &ctx->x_ws,   &ctx->yhat_ws, &ctx->topk_ws, &ctx->inplace.block};
+                                    &ctx->neg_lse, &ctx->x_parts, &ctx->x_ws,   &ctx->yhat_ws, &ctx->topk_ws, &ctx->inplace.block,
+                                    &ctx->attend_ws, &ctx->evict_ws};
   for (pkv::MapperWorkspace& m : ctx->m) {
     DeviceBuffer* b[kLaneBuffers];
     lane_buffers(m, b);
@@ -797,6 +832,42 @@ int proxykv_mask(proxykv_ctx* ctx, const int32_t* idx, int64_t rows, int64_t N, 
   return PROXYKV_OK;
 }
 
+int proxykv_attend(proxykv_ctx* ctx, const void* q, const void* k, const void* v, const int32_t* lens, int32_t dtype, int64_t rows, int64_t N,
+                   int64_t group, int64_t T, int64_t D, void* out, float* weight, void* stream) {
+  if (!ctx || !q || !k || !v || !out) return PROXYKV_EINVAL;
+  if (N <= 0 || N >= (1ll << 31) - 4096 || T > N || D <= 0 || !product_fits({rows, group, T, kAttendQueryUnit})) return PROXYKV_EINVAL;
+  const pkv::AttendArgs a = {q, k, v, nullptr, nullptr, lens, nullptr, out, weight, nullptr, rows, 1, N, 0, group, T, (int)std::min<int64_t>(D, 1 << 20),
+                             dtype == PROXYKV_FP16};
+  return attend_impl(ctx, a, dtype, (hipStream_t)stream);
+}
+
+int proxykv_attend_shared(proxykv_ctx* ctx, const void* q, const void* k_shared, const void* v_shared, const int32_t* shared_lens, const void* k,
+                          const void* v, const int32_t* lens, int32_t dtype, int64_t batch, int64_t heads, int64_t P, int64_t N, int64_t group, int64_t T,
+                          int64_t D, void* out, float* weight_shared, float* weight, void* stream) {
+  if (!ctx || !q || !k_shared || !v_shared || !out || N < 0 || (N > 0 && (!k || !v))) return PROXYKV_EINVAL;
+  if (N >= (1ll << 31) - 4096 || (N > 0 && T > N) || P <= 0 || P >= (1ll << 31) - 4096 || D <= 0 ||
+      !product_fits({batch, heads, group, T, kAttendQueryUnit}))
+    return PROXYKV_EINVAL;
+  const pkv::AttendArgs a = {q, k, v, k_shared, v_shared, lens, shared_lens, out, weight, weight_shared, batch, heads, N, P, group, T,
+                             (int)std::min<int64_t>(D, 1 << 20), dtype == PROXYKV_FP16};
+  return attend_impl(ctx, a, dtype, (hipStream_t)stream);
+}
+
+int proxykv_evict(proxykv_ctx* ctx, void* k, void* v, float* weight, int32_t* positions, int32_t* lens, const int32_t* budgets, int64_t rows,
+                  int64_t N, int64_t budget, int64_t recent, int64_t D, void* stream) {
+  if (!ctx || !k || !v || !weight || !lens) return PROXYKV_EINVAL;
+  if (rows <= 0 || rows >= (1ll << 31) / 1024 || N <= 0 || N >= (1ll << 31) - 4096 || D <= 0 || recent < 0 || recent > N) return PROXYKV_EINVAL;
+  if (!budgets && (budget < 1 || budget > N || recent > budget)) return PROXYKV_EINVAL;
+  if (!aligned(k, 16) || !aligned(v, 16) || !aligned(weight, 4) || !aligned(positions, 4) || !aligned(lens, 4) || !aligned(budgets, 4)) return PROXYKV_EINVAL;
+  if ((D * 2) % 16 != 0 || D * 2 > 512) return PROXYKV_EUNSUPPORTED;
+  hipStream_t s = (hipStream_t)stream;
+  PKV_HIP(ctx, hipSetDevice(ctx->cfg.device));
+  const int rc = ensure_captured(ctx, ctx->evict_ws, pkv::evict_scratch_bytes(rows, N), s);
+  if (rc) return rc;
+  PKV_HIP(ctx, pkv::launch_evict(k, v, weight, positions, lens, budgets, rows, N, budgets ? 0 : budget, recent, D * 2, ctx->evict_ws.ptr, s));
+  return PROXYKV_OK;
+}
+
 int proxykv_prune(proxykv_ctx* ctx, const void* q_rec, const void* k_ctx, const void* k_rec, int32_t dtype, int64_t N,
                   int64_t N_q, int32_t chunk, double keep_ratio, const void* k_in, const void* v_in, void* k_out,
                   void* v_out, int32_t* idx_out, float* x_out, float* yhat_out, int64_t* K_host, void* stream) {
@@ -870,7 +941,7 @@ const char* proxykv_strerror(int status) {
     case PROXYKV_EINVAL: return "invalid argument";
     case PROXYKV_EUNSUPPORTED: return "shape or option not supported by this build";
     case PROXYKV_ENOMEM: return "out of device memory";
-    case PROXYKV_ESTATE: return "context not ready (mapper weights not set)";
+    case PROXYKV_ESTATE: return "context not ready (mapper weights not set, or workspace to be allocated while the stream captures)";
     case PROXYKV_EHIP: return "HIP runtime error";
     case PROXYKV_ELIMIT: return "size beyond a fixed limit of this entry point";
     default: return "unknown status";

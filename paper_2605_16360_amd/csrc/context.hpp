@@ -109,6 +109,7 @@ struct proxykv_ctx {
   pkv::DeviceBuffer x_ws;                          // fp32 [L_s, H_kv, N]
   pkv::DeviceBuffer yhat_ws;                       // fp32 [L_l, H_l, N]
   pkv::DeviceBuffer topk_ws;                       // state of Top-K where workgroups share a row
+  pkv::DeviceBuffer attend_ws, evict_ws;           // shares of a query's softmax; planned moves
   pkv::InplaceCounters inplace;
   bool topk_short = false;                         // memory was short: topk_ws has no masks, or only the narrower histograms
   bool fused_select = false;                       // proxykv_prune: selection and gather in one launch (measured slower)

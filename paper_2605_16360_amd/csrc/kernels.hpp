@@ -75,4 +75,24 @@ hipError_t launch_head_counts(const int32_t* flat, int64_t layers, int64_t heads
                               hipStream_t stream);
 // mask[r, n] = 1 if n is one of idx[r, :], else 0.
 hipError_t launch_mask(const int32_t* idx, int64_t rows, int64_t N, int64_t K, uint8_t* mask, hipStream_t stream);
+
+// Attention of T new tokens of `group` query heads over rows (b, h) of own tokens, k and v [batch, heads, N, D], and over tokens that the
+// batch shares, k_shared and v_shared [heads, P, D] (N or P may be 0, not both); q and out [batch, heads, group, T, D].
+// weight and weight_shared take what every token gets, or are null.
+struct AttendArgs {
+  const void *q, *k, *v, *k_shared, *v_shared;
+  const int32_t *lens, *shared_lens;  // [batch, heads] and [heads] tokens that there are, or null: all
+  void* out;
+  float *weight, *weight_shared;  // [batch, heads, N], [heads, P]
+  int64_t batch, heads, N, P, group, T;
+  int D;
+  bool f16;  // fp16, otherwise bf16
+};
+size_t attend_scratch_bytes(const AttendArgs& a);
+hipError_t launch_attend(const AttendArgs& a, void* scratch, hipStream_t stream);
+
+// Brings every row of more than `budget` (or budgets[r]) tokens back to it (evict.hip).
+size_t evict_scratch_bytes(int64_t rows, int64_t N);
+hipError_t launch_evict(void* k, void* v, float* weight, int32_t* positions, int32_t* lens, const int32_t* budgets, int64_t rows, int64_t N,
+                        int64_t budget, int64_t recent, int64_t row_bytes, void* scratch, hipStream_t stream);
 }  // namespace pkv
