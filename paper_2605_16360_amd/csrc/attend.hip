@@ -1,5 +1,10 @@
 // Attention of new tokens over the compacted cache (what the target does with it after the mask was applied), with an account of the softmax
 // weight that every cached token gets.
+//
+// Three steps.  attend_part_kernel: waves take shares of a row's keys (a row's new tokens are few, its keys many) and leave, for each query, the
+// share's running maximum m, sum l of 2^(c s - m) and unscaled output.  attend_finish_kernel: shares are joined, in order, and where the logits
+// were kept, every key's probabilities are added to the account.  attend_account_kernel: where they were not (many queries), they are
+// computed once more.  No sum's order depends on timing.
 #include "common.hpp"
 #include "kernels.hpp"
 
@@ -7,18 +12,41 @@ namespace pkv {
 namespace {
 
 constexpr float kLog2e = 1.4426950408889634f;
-constexpr float kNone = -__builtin_huge_valf();
+constexpr float kNegInf = -__builtin_huge_valf();
+constexpr float kLow = -1.0e30f;        // a reference below every logit that counts
+constexpr int kTile = 32;               // keys per step of a wave
+constexpr int kXcds = 8;
+constexpr int64_t kKeptQueries = 16;    // up to this many queries per key, logits are kept for the account
 
 template <bool F16>
-__device__ __forceinline__ float to_f32(uint16_t b) {
-  if constexpr (F16) return (float)__builtin_bit_cast(_Float16, b);
-  else return bf16_bits_to_f32(b);
-}
-template <bool F16>
-__device__ __forceinline__ uint16_t from_f32(float f) {
-  if constexpr (F16) return __builtin_bit_cast(uint16_t, (_Float16)f);
-  else return f32_to_bf16_bits(f);
-}
+struct Elem {
+  static __device__ __forceinline__ float wide(uint32_t b) { return F16 ? (float)__builtin_bit_cast(_Float16, (uint16_t)b) : bf16_bits_to_f32((uint16_t)b); }
+  static __device__ __forceinline__ uint16_t narrow(float f) {
+    if constexpr (F16) return __builtin_bit_cast(uint16_t, (_Float16)f);
+    else return f32_to_bf16_bits(f);
+  }
+  static constexpr uint32_t kExp = F16 ? 0x7c00u : 0x7f80u;  // all ones: not finite
+  static __device__ __forceinline__ f32x4 mfma(u32x4 a, u32x4 b, f32x4 c) {
+    if constexpr (F16) return mfma_f16_16x16x32(as_f16x8(a), as_f16x8(b), c);
+    else return mfma_bf16_16x16x32(as_bf16x8(a), as_bf16x8(b), c);
+  }
+  // p as the sums of two 16-bit values: the second holds what the first leaves
+  static __device__ __forceinline__ u32x2 split(float p0, float p1) {
+    uint32_t hi, lo;
+    typedef float f32x2 __attribute__((ext_vector_type(2)));
+    typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
+    typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+    if constexpr (F16) {
+      const f16x2 h = __builtin_convertvector((f32x2{p0, p1}), f16x2);
+      hi = __builtin_bit_cast(uint32_t, h);
+      lo = __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2{p0 - (float)h[0], p1 - (float)h[1]}), f16x2));
+    } else {
+      hi = __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2{p0, p1}), bf16x2));
+      lo = __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2{p0 - __uint_as_float(hi << 16), p1 - __uint_as_float(hi & 0xffff0000u)}), bf16x2));
+    }
+    return {hi, lo};
+  }
+};
 
 // Tokens of a row of `most`: what the device array says, kept inside the row.
 __device__ __forceinline__ int row_len(const int32_t* lens, int64_t row, int64_t most) {
@@ -32,102 +60,519 @@ __device__ __forceinline__ int seen(int len, int T, int t) {
   return n < 0 ? 0 : n;
 }
 
-// One workgroup per query: its waves take 64 keys at a time, a lane one of them, with a running maximum and sum.
-template <int D, bool F16>
-__global__ __launch_bounds__(256) void attend_query_kernel(AttendArgs a, float* __restrict__ lse) {
-  __shared__ float q[D], part_o[4][D], part_m[4], part_l[4];
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  const int64_t query = blockIdx.x, row = query / (a.group * a.T), head = row % a.heads;
-  const int t = (int)(query % a.T);
-  const float c = kLog2e / __builtin_sqrtf((float)D);
-  if (tid < D) q[tid] = to_f32<F16>(((const uint16_t*)a.q)[query * D + tid]);
-  __syncthreads();
-  float m = kNone, l = 0.0f, o[D / 64] = {};
-  auto segment = [&](const uint16_t* k, const uint16_t* v, int n_seen) {
-    for (int n0 = wave * 64; n0 < n_seen; n0 += 256) {
-      const int n = n0 + lane, many = n_seen - n0 < 64 ? n_seen - n0 : 64;
-      float s = kNone;
-      if (n < n_seen) {
-        s = 0.0f;
-        for (int i = 0; i < D; ++i) s = __builtin_fmaf(q[i], to_f32<F16>(k[(size_t)n * D + i]), s);
-        s *= c;
-      }
-      float top = s;
-      for (int off = 32; off; off >>= 1) top = __builtin_fmaxf(top, __shfl_xor(top, off, 64));
-      top = __builtin_fmaxf(top, m);
-      const float p = n < n_seen ? __builtin_amdgcn_exp2f(s - top) : 0.0f, old = l > 0.0f ? __builtin_amdgcn_exp2f(m - top) : 0.0f;
-      float sum = p;
-      for (int off = 32; off; off >>= 1) sum += __shfl_xor(sum, off, 64);
-      m = top;
-      l = l * old + sum;
-      for (int e = 0; e < D / 64; ++e) o[e] *= old;
-      for (int j = 0; j < many; ++j) {
-        const float pj = __shfl(p, j, 64);
-        for (int e = 0; e < D / 64; ++e) o[e] = __builtin_fmaf(pj, to_f32<F16>(v[(size_t)(n0 + j) * D + e * 64 + lane]), o[e]);
+// One kind of keys (shared or own) in a launch: `rows` rows of `n` keys, each seen by m queries, in `tiles` tiles of 16 * ct * waves, and cut into
+// `splits` shares of `chunk` keys.
+struct Keys {
+  int64_t rows, n, m, score_stride;
+  int splits, chunk, tiles, ct, waves, blocks, first_split;
+  float* scores;  // [rows, m, score_stride] logits, or null
+};
+struct Plan {
+  Keys shared, own;
+  int64_t queries;
+  int splits;      // of both kinds together
+  float* ml;       // [splits, queries] pairs
+  float* o;        // [splits, queries, D]
+  float* lse;      // [queries] in the order of q, and behind them in the shared keys' order
+};
+
+// Where query m of a row's m queries lies in q.  Shared keys: row = head, queries (sequence, group head, token).
+__device__ __forceinline__ int64_t query_at(bool shared, int64_t row, int m, int per, int64_t heads) {
+  return shared ? ((int64_t)(m / per) * heads + row) * per + m % per : row * per + m;
+}
+
+template <int D>
+__device__ __forceinline__ int swizzle(int row) { return D == 128 ? row & 15 : (row >> 1) & 7; }
+
+// A step's 16-bit values transposed: fragment d has features 16 d + lane % 16 of keys 4 (lane / 16) + 0..3 and those 16 further on.  `at`: LDS
+// bytes of this lane's piece of fragment 0; the pieces of fragment d lie (d << 5) away by exclusive or, 16 keys further on `next` bytes.  The
+// waits are in the same block as the reads (the compiler, with its own reads, waits for all loads under way as well: they might write there).
+template <int NEXT>
+__device__ __forceinline__ void read_transposed(uint32_t at, int d0, u32x4 (&f)[4]) {
+  u32x2 x[8];
+  asm volatile(
+      "ds_read_b64_tr_b16 %0, %8\n\tds_read_b64_tr_b16 %1, %8 offset:%12\n\t"
+      "ds_read_b64_tr_b16 %2, %9\n\tds_read_b64_tr_b16 %3, %9 offset:%12\n\t"
+      "ds_read_b64_tr_b16 %4, %10\n\tds_read_b64_tr_b16 %5, %10 offset:%12\n\t"
+      "ds_read_b64_tr_b16 %6, %11\n\tds_read_b64_tr_b16 %7, %11 offset:%12\n\t"
+      "s_waitcnt lgkmcnt(0)"
+      : "=&v"(x[0]), "=&v"(x[1]), "=&v"(x[2]), "=&v"(x[3]), "=&v"(x[4]), "=&v"(x[5]), "=&v"(x[6]), "=&v"(x[7])
+      : "v"(at ^ (uint32_t)(d0 << 5)), "v"(at ^ (uint32_t)((d0 + 1) << 5)), "v"(at ^ (uint32_t)((d0 + 2) << 5)), "v"(at ^ (uint32_t)((d0 + 3) << 5)),
+        "n"(NEXT)
+      : "memory");
+#pragma unroll
+  for (int i = 0; i < 4; ++i) f[i] = u32x4{x[2 * i][0], x[2 * i][1], x[2 * i + 1][0], x[2 * i + 1][1]};
+}
+
+// A block's share: keys [begin, end) of a row for 16 * CT * W queries, of which each of the W waves has 16 * CT.  The waves share the keys' tiles.
+template <int D, bool F16, int CT, int W>
+struct Part {
+  using E = Elem<F16>;
+  static constexpr int CPR = D / 8, KK = D / 32, DT = D / 16;  // 16-byte pieces per key; products' steps; output tiles
+  static constexpr int NL = kTile * CPR / 64;                  // a tile's loads of K, by a wave
+  static constexpr int STAGES = W == 1 ? 2 : 3, STAGE = 2 * NL * 64;
+  static constexpr int MINE = 2 * NL / W;                      // loads of a wave per tile
+  static_assert(MINE * W == 2 * NL, "the waves share a tile's loads");
+
+  static __device__ __forceinline__ void run(const AttendArgs& a, const Plan& p, const Keys& ks, bool shared, int64_t row, int split, int tile0, u32x4* lds) {
+    const int lane = threadIdx.x & 63, wave = W == 1 ? 0 : __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), col = lane & 15, quad = lane >> 4;
+    const int per = (int)(a.group * a.T), T = (int)a.T, M = (int)ks.m;
+    const int b0 = tile0 * 16 * CT * W, m0 = b0 + wave * 16 * CT;
+    const float c = kLog2e / __builtin_sqrtf((float)D);
+    const int len = row_len(shared ? a.shared_lens : a.lens, row, ks.n);
+    // keys that all, and that any, of the block's (most) and of the wave's queries (least) see
+    int64_t query[CT];
+    int see[CT];
+    int least = len, most = len;
+#pragma unroll
+    for (int ct = 0; ct < CT; ++ct) {
+      const int m = m0 + ct * 16 + col, mc = m < M ? m : M - 1;
+      query[ct] = query_at(shared, row, mc, per, a.heads);
+      see[ct] = shared ? len : seen(len, T, mc % T);
+    }
+    if (!shared) {
+      const int b1 = (b0 + 16 * CT * W < M ? b0 + 16 * CT * W : M) - 1, w0 = m0 < M ? m0 : M - 1, w1 = (m0 + 16 * CT < M ? m0 + 16 * CT : M) - 1;
+      most = seen(len, T, b0 / T == b1 / T ? b1 % T : T - 1);  // (tokens of one head, in order)
+      least = seen(len, T, w0 / T == w1 / T ? w0 % T : 0);
+    }
+    const int begin = split * ks.chunk, end = begin + ks.chunk < most ? begin + ks.chunk : most;
+    const int n_tiles = end > begin ? (end - begin + kTile - 1) / kTile : 0;
+
+    float m_run[CT], l_run[CT];
+    f32x4 o[DT][CT];
+#pragma unroll
+    for (int ct = 0; ct < CT; ++ct) {
+      m_run[ct] = kLow;
+      l_run[ct] = 0.0f;
+#pragma unroll
+      for (int d = 0; d < DT; ++d) o[d][ct] = f32x4{0, 0, 0, 0};
+    }
+    if (n_tiles > 0) {
+      u32x4 bq[CT][KK];
+#pragma unroll
+      for (int ct = 0; ct < CT; ++ct)
+#pragma unroll
+        for (int kk = 0; kk < KK; ++kk) bq[ct][kk] = *reinterpret_cast<const u32x4*>((const uint16_t*)a.q + query[ct] * D + kk * 32 + quad * 8);
+      const uint8_t* kb = (const uint8_t*)(shared ? a.k_shared : a.k) + ((size_t)row * ks.n + begin) * (D * 2);
+      const uint8_t* vb = (const uint8_t*)(shared ? a.v_shared : a.v) + ((size_t)row * ks.n + begin) * (D * 2);
+      typedef const __attribute__((address_space(1))) void* gptr_t;
+      typedef __attribute__((address_space(3))) void* lptr_t;
+      // Tile t straight into LDS, a key's pieces exchanged (swizzle) so that fragments are read from all banks.  Keys behind the last are the
+      // last one again: nothing behind it is touched.
+      auto fetch = [&](int t, int stage) __attribute__((always_inline)) {
+        u32x4* st = lds + stage * STAGE;
+        const int last = end - 1 - begin - t * kTile;
+        const uint8_t *kt = kb + (size_t)t * (kTile * D * 2), *vt = vb + (size_t)t * (kTile * D * 2);
+#pragma unroll
+        for (int i = 0; i < MINE; ++i) {
+          const int j = wave * MINE + i, jk = j < NL ? j : j - NL;  // piece j: NL of K, then NL of V
+          const int r = jk * (64 / CPR) + lane / CPR, at = (r < last ? r : last) * (D * 2) + ((lane % CPR) ^ swizzle<D>(r)) * 16;
+          __builtin_amdgcn_global_load_lds((gptr_t)((j < NL ? kt : vt) + at), (lptr_t)(st + j * 64), 16, 0, 0);
+        }
+      };
+      auto tile = [&](int t, const u32x4* st, auto cut_c) __attribute__((always_inline)) {
+        constexpr bool cut = decltype(cut_c)::value;
+        const int n0 = begin + t * kTile;
+        // S^T: a lane has the logits of its query (column) with keys 4 quad + r and 16 + 4 quad + r
+        f32x4 s[2][CT];
+#pragma unroll
+        for (int kt = 0; kt < 2; ++kt) {
+          u32x4 f[KK];
+#pragma unroll
+          for (int kk = 0; kk < KK; ++kk) {
+            const int r = kt * 16 + col;
+            f[kk] = st[r * CPR + ((kk * 4 + quad) ^ swizzle<D>(r))];
+          }
+#pragma unroll
+          for (int ct = 0; ct < CT; ++ct) s[kt][ct] = f32x4{0, 0, 0, 0};
+#pragma unroll
+          for (int kk = 0; kk < KK; ++kk)
+#pragma unroll
+            for (int ct = 0; ct < CT; ++ct) s[kt][ct] = E::mfma(f[kk], bq[ct][kk], s[kt][ct]);
+        }
+        if (W == 1 && ks.scores != nullptr) {
+#pragma unroll
+          for (int ct = 0; ct < CT; ++ct) {
+            const int m = m0 + ct * 16 + col;
+            if (m < M) {
+              float* at = ks.scores + ((size_t)row * M + m) * ks.score_stride + n0 + quad * 4;
+              *reinterpret_cast<f32x4*>(at) = s[0][ct];
+              *reinterpret_cast<f32x4*>(at + 16) = s[1][ct];
+            }
+          }
+        }
+        u32x4 hi[CT], lo[CT];
+        float pf[CT][8];
+#pragma unroll
+        for (int ct = 0; ct < CT; ++ct) {
+          float x[8];
+#pragma unroll
+          for (int i = 0; i < 8; ++i) {
+            x[i] = s[i >> 2][ct][i & 3];
+            if constexpr (cut) x[i] = n0 + (i >> 2) * 16 + quad * 4 + (i & 3) < see[ct] ? x[i] : kNegInf;
+          }
+          float top = max3f(x[0], x[1], x[2]);
+          top = max3f(top, x[3], x[4]);
+          top = max3f(top, x[5], x[6]);
+          top = quads_max(__builtin_fmaxf(top, x[7])) * c;
+          // the reference moves only where a logit lies 2^8 above it: probabilities up to that lose nothing
+          if (__builtin_amdgcn_ballot_w64(top > m_run[ct] + 8.0f)) {
+            const float m = __builtin_fmaxf(m_run[ct], top), f = __builtin_amdgcn_exp2f(m_run[ct] - m);
+            m_run[ct] = m;
+            l_run[ct] *= f;
+#pragma unroll
+            for (int d = 0; d < DT; ++d) o[d][ct] *= f;
+          }
+          float sum = 0.0f;
+#pragma unroll
+          for (int i = 0; i < 8; ++i) {
+            pf[ct][i] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[i], c, -m_run[ct]));
+            sum += pf[ct][i];
+          }
+          l_run[ct] += sum;
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const u32x2 x2 = E::split(pf[ct][2 * i], pf[ct][2 * i + 1]);
+            hi[ct][i] = x2[0];
+            lo[ct][i] = x2[1];
+          }
+        }
+        // O^T += V^T P^T: 16 features by the keys that the lane's probabilities belong to
+        const u32x4* vst = st + NL * 64;
+        const int vr = quad * 4 + (col >> 2);
+        const uint32_t at = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) const void*)(vst + vr * CPR + (((col >> 1) & 1) ^ swizzle<D>(vr))) + (col & 1) * 8;
+        bool bad = false;
+#pragma unroll
+        for (int d0 = 0; d0 < DT; d0 += 4) {
+          u32x4 v[4];
+          read_transposed<16 * D * 2>(at, d0, v);
+          if constexpr (cut) {
+            // values that are not finite must not meet the zero probabilities of queries that do not see them
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+              const uint32_t x = v[i >> 2][i & 3];
+              const bool x0 = (x & E::kExp) == E::kExp, x1 = (x >> 16 & E::kExp) == E::kExp;
+              bad = bad || x0 || x1;
+              v[i >> 2][i & 3] = x & ((x0 ? 0u : 0xffffu) | (x1 ? 0u : 0xffff0000u));
+            }
+          }
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+#pragma unroll
+            for (int ct = 0; ct < CT; ++ct) o[d0 + i][ct] = E::mfma(v[i], hi[ct], o[d0 + i][ct]);
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+#pragma unroll
+            for (int ct = 0; ct < CT; ++ct) o[d0 + i][ct] = E::mfma(v[i], lo[ct], o[d0 + i][ct]);
+        }
+        if constexpr (cut) {
+          if (__builtin_amdgcn_ballot_w64(bad)) {  // they meet those that do, one by one
+#pragma unroll
+            for (int ct = 0; ct < CT; ++ct)
+#pragma unroll
+              for (int i = 0; i < 8; ++i)
+#pragma unroll 1
+                for (int qd = 0; qd < 4; ++qd) {
+                  const int j = (i >> 2) * 16 + qd * 4 + (i & 3);
+                  const float pj = __shfl(pf[ct][i], qd * 16 + col, 64);
+                  const bool sees = n0 + j < see[ct];
+#pragma unroll
+                  for (int d = 0; d < DT; ++d) {
+                    const int f = d * 16 + quad * 4;
+                    const u32x2 y = *reinterpret_cast<const u32x2*>((const uint16_t*)(vst + j * CPR + ((f >> 3) ^ swizzle<D>(j))) + (f & 7));
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                      const uint32_t x = e & 1 ? y[e >> 1] >> 16 : y[e >> 1] & 0xffffu;
+                      if (sees && (x & E::kExp) == E::kExp) o[d][ct][e] = __builtin_fmaf(pj, E::wide(x), o[d][ct][e]);
+                    }
+                  }
+                }
+          }
+        }
+      };
+      fetch(0, 0);
+      if (n_tiles > 1) fetch(1, 1);
+      int stage = 0;
+      for (int t = 0; t < n_tiles; ++t) {
+        // this wave's part of tile t has landed; its loads of tile t + 1 may be under way
+        if (t + 1 < n_tiles) __builtin_amdgcn_s_waitcnt(MINE == 16 ? 0x4F70 : 0x0F70 | MINE);
+        else __builtin_amdgcn_s_waitcnt(0x0F70);
+        asm volatile("" ::: "memory");
+        if constexpr (W > 1) {
+          __builtin_amdgcn_s_barrier();  // everyone's has, and everyone has read tile t - 1, whose place takes tile t + 2
+          asm volatile("" ::: "memory");
+          if (t + 2 < n_tiles) fetch(t + 2, stage == 0 ? 2 : stage - 1);
+        }
+        const u32x4* st = lds + stage * STAGE;
+        if (begin + (t + 1) * kTile <= least && begin + (t + 1) * kTile <= end) tile(t, st, std::integral_constant<bool, false>{});
+        else tile(t, st, std::integral_constant<bool, true>{});
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // all of tile t has been read
+        if (W == 1 && t + 2 < n_tiles) fetch(t + 2, stage);
+        stage = stage == STAGES - 1 ? 0 : stage + 1;
       }
     }
+    const size_t at = (size_t)(ks.first_split + split) * p.queries;
+#pragma unroll
+    for (int ct = 0; ct < CT; ++ct) {
+      const float l = quads_sum(l_run[ct]);
+      if (m0 + ct * 16 + col < M) {
+        if (quad == 0) reinterpret_cast<float2*>(p.ml)[at + query[ct]] = float2{m_run[ct], l};
+        if (n_tiles > 0) {
+#pragma unroll
+          for (int d = 0; d < DT; ++d) *reinterpret_cast<f32x4*>(p.o + (at + query[ct]) * D + d * 16 + quad * 4) = o[d][ct];
+        }
+      }
+    }
+  }
+};
+
+// Blocks that share keys (tiles of one row's queries) follow each other on one XCD, whose L2 then has the keys.
+// false: nothing to do
+__device__ __forceinline__ bool share_of(int b, const Keys& ks, int64_t& row, int& split, int& tile) {
+  const int64_t share = (int64_t)(b / (kXcds * ks.tiles)) * kXcds + b % kXcds;
+  tile = b / kXcds % ks.tiles;
+  row = share / ks.splits;
+  split = (int)(share % ks.splits);
+  return share < ks.rows * ks.splits;
+}
+
+// Few queries per row: a wave each.  CT: of the kind of keys that has the larger tiles.
+template <int D, bool F16, int CT>
+__global__ __launch_bounds__(64, 1) void attend_wave_kernel(AttendArgs a, Plan p) {
+  __shared__ u32x4 lds[Part<D, F16, CT, 1>::STAGES * Part<D, F16, CT, 1>::STAGE];
+  const bool shared = (int)blockIdx.x < p.shared.blocks;
+  const Keys& ks = shared ? p.shared : p.own;
+  int64_t row;
+  int split, tile;
+  if (!share_of(shared ? blockIdx.x : blockIdx.x - p.shared.blocks, ks, row, split, tile)) return;
+  if (CT == 1 || ks.ct == 1) Part<D, F16, 1, 1>::run(a, p, ks, shared, row, split, tile, lds);
+  else Part<D, F16, CT, 1>::run(a, p, ks, shared, row, split, tile, lds);
+}
+
+// Many: W waves of 32 queries share the keys.
+template <int D, bool F16, int W>
+__global__ __launch_bounds__(64 * W, W < 4 ? 1 : W / 4) void attend_block_kernel(AttendArgs a, Plan p, bool shared) {
+  __shared__ u32x4 lds[Part<D, F16, 2, W>::STAGES * Part<D, F16, 2, W>::STAGE];
+  const Keys& ks = shared ? p.shared : p.own;
+  int64_t row;
+  int split, tile;
+  if (!share_of(blockIdx.x, ks, row, split, tile)) return;
+  Part<D, F16, 2, W>::run(a, p, ks, shared, row, split, tile, lds);
+}
+
+// (m, l) of a query's shares joined, by a wave: 2^m l is the sum of all
+struct Joined {
+  float m, l;
+};
+__device__ __forceinline__ Joined join(const float* ml, int64_t query, int64_t queries, int splits, int lane) {
+  float m = kLow, l = 0.0f;
+  for (int s0 = 0; s0 < splits; s0 += 64) {
+    const int s = s0 + lane;
+    const float2 x = s < splits ? reinterpret_cast<const float2*>(ml)[(size_t)s * queries + query] : float2{kLow, 0.0f};
+    float top = x.x;
+    for (int off = 32; off; off >>= 1) top = __builtin_fmaxf(top, __shfl_xor(top, off, 64));
+    top = __builtin_fmaxf(m, top);
+    float sum = x.y * __builtin_amdgcn_exp2f(x.x - top);
+    for (int off = 32; off; off >>= 1) sum += __shfl_xor(sum, off, 64);
+    l = l * __builtin_amdgcn_exp2f(m - top) + sum;
+    m = top;
+  }
+  return {m, l};
+}
+
+// Blocks below `query_blocks`: four queries each, a wave for one: the shares' outputs joined.  The others: the account of 1024 keys of a row.
+template <int D, bool F16>
+__global__ __launch_bounds__(256) void attend_finish_kernel(AttendArgs a, Plan p, int query_blocks, int shared_blocks) {
+  __shared__ float lse[kKeptQueries];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, per = (int)(a.group * a.T);
+  if ((int)blockIdx.x < query_blocks) {
+    const int64_t query = (int64_t)blockIdx.x * 4 + wave;
+    if (query >= p.queries) return;
+    const Joined j = join(p.ml, query, p.queries, p.splits, lane);
+    float x[D / 64] = {};
+    for (int s = 0; s < p.splits; ++s) {
+      const float2 ml = reinterpret_cast<const float2*>(p.ml)[(size_t)s * p.queries + query];
+      const float f = __builtin_amdgcn_exp2f(ml.x - j.m);
+      if (ml.y != 0.0f) {
+        const float* o = p.o + ((size_t)s * p.queries + query) * D + lane * (D / 64);
+#pragma unroll
+        for (int e = 0; e < D / 64; ++e) x[e] = __builtin_fmaf(f, o[e], x[e]);
+      }
+    }
+    const bool none = j.l == 0.0f;
+#pragma unroll
+    for (int e = 0; e < D / 64; ++e) ((uint16_t*)a.out)[query * D + lane * (D / 64) + e] = Elem<F16>::narrow(none ? 0.0f : x[e] / j.l);
+    if (lane == 0 && p.lse != nullptr) {
+      const float v = none ? -kNegInf : j.m + __builtin_amdgcn_logf(j.l);
+      p.lse[query] = v;
+      const int64_t row = query / per;  // (sequence, head)
+      p.lse[p.queries + (row % a.heads * a.batch + row / a.heads) * per + query % per] = v;
+    }
+    return;
+  }
+  int b = blockIdx.x - query_blocks;
+  const bool shared = b < shared_blocks;
+  if (!shared) b -= shared_blocks;
+  const Keys& ks = shared ? p.shared : p.own;
+  const int blocks = (int)((ks.n + 1023) / 1024), n0 = b % blocks * 1024, M = (int)ks.m, T = (int)a.T;
+  const int64_t row = b / blocks;
+  const int len = row_len(shared ? a.shared_lens : a.lens, row, ks.n);
+  if (n0 >= len) return;
+  for (int m = wave; m < M; m += 4) {
+    const Joined j = join(p.ml, query_at(shared, row, m, per, a.heads), p.queries, p.splits, lane);
+    if (lane == 0) lse[m] = j.l == 0.0f ? -kNegInf : j.m + __builtin_amdgcn_logf(j.l);
+  }
+  __syncthreads();
+  const float c = kLog2e / __builtin_sqrtf((float)D);
+  float* w = (shared ? a.weight_shared : a.weight) + row * ks.n;
+  for (int n = n0 + threadIdx.x; n < n0 + 1024 && n < len; n += 256) {
+    float sum = 0.0f;
+    for (int m = 0; m < M; ++m) {
+      const float s = ks.scores[((size_t)row * M + m) * ks.score_stride + n];
+      sum += shared || n < seen(len, T, m % T) ? __builtin_amdgcn_exp2f(__builtin_fmaf(s, c, -lse[m])) : 0.0f;
+    }
+    w[n] += sum;
+  }
+}
+
+// The account where the logits were not kept: a wave holds 64 keys and walks the queries that see them, 16 at a time.  S: a lane has the
+// logits of its key (column) with queries 4 quad + r.
+template <int D, bool F16>
+__global__ __launch_bounds__(256) void attend_account_kernel(AttendArgs a, Keys ks, bool shared, const float* __restrict__ lse) {
+  using E = Elem<F16>;
+  constexpr int KK = D / 32;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, col = lane & 15, quad = lane >> 4;
+  const int per = (int)(a.group * a.T), T = (int)a.T, M = (int)ks.m, blocks = (int)((ks.n + 255) / 256);
+  const int64_t row = blockIdx.x / blocks;
+  const int n0 = blockIdx.x % blocks * 256 + wave * 64;
+  const int len = row_len(shared ? a.shared_lens : a.lens, row, ks.n);
+  if (n0 >= len) return;
+  const float c = kLog2e / __builtin_sqrtf((float)D);
+  u32x4 bk[4][KK];
+#pragma unroll
+  for (int kt = 0; kt < 4; ++kt) {
+    const int n = n0 + kt * 16 + col;
+    const uint16_t* k = (const uint16_t*)(shared ? a.k_shared : a.k) + ((size_t)row * ks.n + (n < len ? n : len - 1)) * D + quad * 8;
+#pragma unroll
+    for (int kk = 0; kk < KK; ++kk) bk[kt][kk] = *reinterpret_cast<const u32x4*>(k + kk * 32);
+  }
+  float sum[4] = {};
+  for (int q0 = 0; q0 < M; q0 += 16) {
+    const int mq = q0 + col < M ? q0 + col : M - 1;
+    const uint16_t* q = (const uint16_t*)a.q + query_at(shared, row, mq, per, a.heads) * D + quad * 8;
+    u32x4 fq[KK];
+#pragma unroll
+    for (int kk = 0; kk < KK; ++kk) fq[kk] = *reinterpret_cast<const u32x4*>(q + kk * 32);
+    float ref[4];
+    int see[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const int m = q0 + quad * 4 + e;
+      ref[e] = m < M ? lse[row * M + m] : -kNegInf;
+      see[e] = shared ? len : seen(len, T, m % T);
+    }
+#pragma unroll
+    for (int kt = 0; kt < 4; ++kt) {
+      f32x4 s = {0, 0, 0, 0};
+#pragma unroll
+      for (int kk = 0; kk < KK; ++kk) s = E::mfma(fq[kk], bk[kt][kk], s);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) sum[kt] += n0 + kt * 16 + col < see[e] ? __builtin_amdgcn_exp2f(__builtin_fmaf(s[e], c, -ref[e])) : 0.0f;
+    }
+  }
+  float* w = (shared ? a.weight_shared : a.weight) + row * ks.n;
+#pragma unroll
+  for (int kt = 0; kt < 4; ++kt) {
+    const float x = quads_sum(sum[kt]);
+    const int n = n0 + kt * 16 + col;
+    if (quad == 0 && n < len) w[n] += x;
+  }
+}
+
+// Shares of at least kLeastKeys keys, as many as give the chip kWaves waves of this kind.
+constexpr int64_t kLeastKeys = 256, kWaves = 2048;
+
+Keys keys_of(int64_t rows, int64_t n, int64_t m, bool account) {
+  Keys k = {};
+  k.rows = rows;
+  k.n = n;
+  k.m = m;
+  if (n == 0) {
+    k.tiles = 1;
+    return k;
+  }
+  k.ct = m <= 16 ? 1 : 2;
+  k.waves = m <= 32 ? 1 : m <= 64 ? 2 : m <= 128 ? 4 : 8;
+  const int64_t tile = 16 * k.ct * k.waves;
+  k.tiles = (int)((m + tile - 1) / tile);
+  int64_t splits = (kWaves + rows * k.tiles * k.waves - 1) / (rows * k.tiles * k.waves);
+  const int64_t most = (n + kLeastKeys - 1) / kLeastKeys;
+  splits = splits < most ? splits : most;
+  k.chunk = (int)(((n + splits - 1) / splits + kTile - 1) / kTile * kTile);
+  k.splits = (int)((n + k.chunk - 1) / k.chunk);
+  k.blocks = (int)((rows * k.splits + kXcds - 1) / kXcds * kXcds * k.tiles);
+  k.score_stride = account && m <= kKeptQueries ? (n + kTile - 1) / kTile * kTile : 0;
+  return k;
+}
+
+size_t plan_of(const AttendArgs& a, Plan* out, uint8_t* scratch) {
+  const int64_t per = a.group * a.T, rows = a.batch * a.heads;
+  Plan p = {};
+  p.queries = rows * per;
+  p.shared = keys_of(a.heads, a.P, a.batch * per, a.weight_shared != nullptr);
+  p.own = keys_of(rows, a.N, per, a.weight != nullptr);
+  p.own.first_split = p.shared.splits;
+  p.splits = p.shared.splits + p.own.splits;
+  size_t at = 0;
+  auto take = [&](size_t floats) {
+    float* r = (float*)(scratch + at);
+    at += (floats * 4 + 255) / 256 * 256;
+    return r;
   };
-  if (a.P > 0)
-    segment((const uint16_t*)a.k_shared + (size_t)head * a.P * D, (const uint16_t*)a.v_shared + (size_t)head * a.P * D, row_len(a.shared_lens, head, a.P));
-  if (a.N > 0) segment((const uint16_t*)a.k + (size_t)row * a.N * D, (const uint16_t*)a.v + (size_t)row * a.N * D, seen(row_len(a.lens, row, a.N), (int)a.T, t));
-  for (int e = 0; e < D / 64; ++e) part_o[wave][e * 64 + lane] = o[e];
-  if (lane == 0) {
-    part_m[wave] = m;
-    part_l[wave] = l;
-  }
-  __syncthreads();
-  float top = part_m[0], sum = 0.0f, f[4];
-  for (int w = 1; w < 4; ++w) top = __builtin_fmaxf(top, part_m[w]);
-  for (int w = 0; w < 4; ++w) {
-    f[w] = part_l[w] != 0.0f ? __builtin_amdgcn_exp2f(part_m[w] - top) : 0.0f;
-    sum += f[w] * part_l[w];
-  }
-  const bool none = sum == 0.0f;
-  if (tid < D) {
-    float x = 0.0f;
-    for (int w = 0; w < 4; ++w) x += f[w] * part_o[w][tid];
-    ((uint16_t*)a.out)[query * D + tid] = from_f32<F16>(none ? 0.0f : x / sum);
-  }
-  if (tid == 0 && lse != nullptr) lse[query] = none ? -kNone : top + __builtin_amdgcn_logf(sum);
-}
-
-// weight[n] += sum over the queries that see key n of 2^(c <q, k_n> - lse).  One thread per key; shared keys are seen by every
-// sequence's queries of their head, own ones by their row's.
-template <int D, bool F16, bool SHARED>
-__global__ __launch_bounds__(256) void attend_weight_kernel(AttendArgs a, const float* __restrict__ lse) {
-  const int64_t row = blockIdx.y + (int64_t)blockIdx.z * gridDim.y, rows = SHARED ? a.heads : a.batch * a.heads;
-  if (row >= rows) return;
-  const int64_t most = SHARED ? a.P : a.N;
-  const int len = row_len(SHARED ? a.shared_lens : a.lens, row, most), n = blockIdx.x * 256 + threadIdx.x, T = (int)a.T;
-  if (n >= len) return;
-  const uint16_t* k = (const uint16_t*)(SHARED ? a.k_shared : a.k) + ((size_t)row * most + n) * D;
-  const float c = kLog2e / __builtin_sqrtf((float)D);
-  const int64_t per = a.group * a.T;
-  float w = 0.0f;
-  for (int64_t b = 0; b < (SHARED ? a.batch : 1); ++b)
-    for (int64_t g = 0; g < per; ++g) {
-      const int64_t query = (SHARED ? b * a.heads + row : row) * per + g;
-      if (!SHARED && n >= seen(len, T, (int)(g % T))) continue;
-      const uint16_t* q = (const uint16_t*)a.q + query * D;
-      float s = 0.0f;
-      for (int i = 0; i < D; ++i) s = __builtin_fmaf(to_f32<F16>(q[i]), to_f32<F16>(k[i]), s);
-      w += __builtin_amdgcn_exp2f(c * s - lse[query]);
-    }
-  (SHARED ? a.weight_shared : a.weight)[row * most + n] += w;
+  p.ml = take((size_t)p.splits * p.queries * 2);
+  p.o = take((size_t)p.splits * p.queries * a.D);
+  p.lse = take((size_t)p.queries * 2);
+  if (p.shared.score_stride) p.shared.scores = take((size_t)(p.shared.rows * p.shared.m * p.shared.score_stride));
+  if (p.own.score_stride) p.own.scores = take((size_t)(p.own.rows * p.own.m * p.own.score_stride));
+  if (out) *out = p;
+  return at;
 }
 
 template <int D, bool F16>
-hipError_t launch_attend_of(const AttendArgs& a, float* lse, hipStream_t stream) {
-  const int64_t rows = a.batch * a.heads;
-  attend_query_kernel<D, F16><<<(unsigned)(rows * a.group * a.T), 256, 0, stream>>>(a, lse);
-  hipError_t e = hipGetLastError();
-  auto grid = [](int64_t n, int64_t r) { return dim3((unsigned)((n + 255) / 256), (unsigned)(r < 65535 ? r : 65535), (unsigned)((r + 65534) / 65535)); };
-  if (e == hipSuccess && a.weight != nullptr && a.N > 0) {
-    attend_weight_kernel<D, F16, false><<<grid(a.N, rows), 256, 0, stream>>>(a, lse);
+hipError_t launch_attend_of(const AttendArgs& a, void* scratch, hipStream_t stream) {
+  Plan p;
+  plan_of(a, &p, (uint8_t*)scratch);
+  hipError_t e = hipSuccess;
+  auto many = [&](const Keys& k, bool shared) {
+    if (e != hipSuccess || k.waves <= 1) return;
+    if (k.waves == 2) attend_block_kernel<D, F16, 2><<<(unsigned)k.blocks, 128, 0, stream>>>(a, p, shared);
+    else if (k.waves == 4) attend_block_kernel<D, F16, 4><<<(unsigned)k.blocks, 256, 0, stream>>>(a, p, shared);
+    else attend_block_kernel<D, F16, 8><<<(unsigned)k.blocks, 512, 0, stream>>>(a, p, shared);
+    e = hipGetLastError();
+  };
+  many(p.shared, true);
+  many(p.own, false);
+  Plan few = p;
+  if (p.shared.waves > 1) few.shared.blocks = 0;
+  if (p.own.waves > 1) few.own.blocks = 0;
+  const unsigned blocks = (unsigned)(few.shared.blocks + few.own.blocks);
+  if (e == hipSuccess && blocks > 0) {
+    if ((few.shared.blocks && p.shared.ct == 2) || (few.own.blocks && p.own.ct == 2)) attend_wave_kernel<D, F16, 2><<<blocks, 64, 0, stream>>>(a, few);
+    else attend_wave_kernel<D, F16, 1><<<blocks, 64, 0, stream>>>(a, few);
     e = hipGetLastError();
   }
-  if (e == hipSuccess && a.weight_shared != nullptr && a.P > 0) {
-    attend_weight_kernel<D, F16, true><<<grid(a.P, a.heads), 256, 0, stream>>>(a, lse);
+  if (e != hipSuccess) return e;
+  const int query_blocks = (int)((p.queries + 3) / 4);
+  const int64_t shared_blocks = p.shared.scores ? p.shared.rows * ((p.shared.n + 1023) / 1024) : 0;
+  const int64_t own_blocks = p.own.scores ? p.own.rows * ((p.own.n + 1023) / 1024) : 0;
+  attend_finish_kernel<D, F16><<<(unsigned)(query_blocks + shared_blocks + own_blocks), 256, 0, stream>>>(a, p, query_blocks, (int)shared_blocks);
+  e = hipGetLastError();
+  if (e == hipSuccess && a.weight_shared != nullptr && !p.shared.scores) {
+    attend_account_kernel<D, F16><<<(unsigned)(p.shared.rows * ((p.shared.n + 255) / 256)), 256, 0, stream>>>(a, p.shared, true, p.lse + p.queries);
+    e = hipGetLastError();
+  }
+  if (e == hipSuccess && a.weight != nullptr && p.own.n > 0 && !p.own.scores) {
+    attend_account_kernel<D, F16><<<(unsigned)(p.own.rows * ((p.own.n + 255) / 256)), 256, 0, stream>>>(a, p.own, false, p.lse);
     e = hipGetLastError();
   }
   return e;
@@ -135,11 +580,11 @@ hipError_t launch_attend_of(const AttendArgs& a, float* lse, hipStream_t stream)
 
 }  // namespace
 
-size_t attend_scratch_bytes(const AttendArgs& a) { return (size_t)(a.batch * a.heads * a.group * a.T) * 4; }
+size_t attend_scratch_bytes(const AttendArgs& a) { return plan_of(a, nullptr, nullptr); }
 
 hipError_t launch_attend(const AttendArgs& a, void* scratch, hipStream_t stream) {
-  if (a.D == 64) return a.f16 ? launch_attend_of<64, true>(a, (float*)scratch, stream) : launch_attend_of<64, false>(a, (float*)scratch, stream);
-  return a.f16 ? launch_attend_of<128, true>(a, (float*)scratch, stream) : launch_attend_of<128, false>(a, (float*)scratch, stream);
+  if (a.D == 64) return a.f16 ? launch_attend_of<64, true>(a, scratch, stream) : launch_attend_of<64, false>(a, scratch, stream);
+  return a.f16 ? launch_attend_of<128, true>(a, scratch, stream) : launch_attend_of<128, false>(a, scratch, stream);
 }
 
 }  // namespace pkv
