@@ -145,6 +145,7 @@ class Context:
 
     def __init__(self, cfg: proxykv_config):
         self.cfg = cfg
+        self.device = cfg.device
         self.handle = ctypes.c_void_p()
         _check(load().proxykv_create(ctypes.byref(self.handle), ctypes.byref(cfg)), "proxykv_create")
 
@@ -232,9 +233,11 @@ def _stream_ptr(stream) -> Optional[int]:
     return stream.cuda_stream or None
 
 
-def _stream_on(ctx: Context, stream) -> Optional[int]:
+def _stream_on(device: int, stream) -> Optional[int]:
     """The stream's handle; without one, that of the current stream of the context's device, whatever the current device is."""
-    return _stream_ptr(torch.cuda.current_stream(ctx.cfg.device) if stream is None else stream)
+    if stream is not None:
+        return stream.cuda_stream or None
+    return torch._C._cuda_getCurrentRawStream(device) or None  # (torch.cuda.current_stream makes an object of it first: 2 us)
 
 
 def _qk_dtype(q: torch.Tensor) -> int:
@@ -362,40 +365,40 @@ def proxykv_compact_pooled(ctx: Context, k, v, flat, counts, stream=None) -> Non
            "proxykv_compact_pooled", ctx.handle)
 
 
-def _on_device(ctx: Context, **tensors) -> None:
-    for name, t in tensors.items():
-        if t is not None and (not t.is_cuda or t.device.index != ctx.cfg.device):
-            raise ValueError(f"{name} must be on the context's device cuda:{ctx.cfg.device}, not {t.device}")
-
-
-def _expect(name: str, t: Optional[torch.Tensor], shape, dtype) -> None:
-    if t is not None and (tuple(t.shape) != tuple(shape) or t.dtype != dtype):
+def _arg(name: str, t: Optional[torch.Tensor], device: int, dtype, shape) -> Optional[int]:
+    """A tensor's address, behind the checks that every tensor of the decode calls has to pass."""
+    if t is None:
+        return None
+    if t.get_device() != device:
+        raise ValueError(f"{name} must be on the context's device cuda:{device}, not {t.device}")
+    if t.dtype != dtype or t.shape != shape:
         raise ValueError(f"{name} must be {dtype} {tuple(shape)}, got {t.dtype} {tuple(t.shape)}")
+    if not t.is_contiguous():
+        raise ValueError(f"{name} must be contiguous")
+    return t.data_ptr()
+
+
+_CACHE_DTYPES = {torch.bfloat16: PROXYKV_BF16, torch.float16: PROXYKV_FP16}
 
 
 def _cache_dtype(q: torch.Tensor) -> int:
-    if q.dtype == torch.bfloat16:
-        return PROXYKV_BF16
-    if q.dtype == torch.float16:
-        return PROXYKV_FP16
-    raise ValueError("the cache and its queries must be bf16 or fp16")
+    if q.dtype not in _CACHE_DTYPES:
+        raise ValueError("the cache and its queries must be bf16 or fp16")
+    return _CACHE_DTYPES[q.dtype]
 
 
 def proxykv_attend(ctx: Context, q, k, v, lens=None, weight=None, out=None, stream=None) -> torch.Tensor:
     """Attention of new tokens over a layer's cache: q [..., group, T, D], k and v [..., N, D], lens int32 [...] tokens per row (None: N);
     weight fp32 [..., N], if given, is added every token's probabilities.  The leading dimensions are the rows."""
-    (group, T, D), N, rows = q.shape[-3:], k.shape[-2], q.shape[:-3]
-    _on_device(ctx, q=q, k=k, v=v, lens=lens, weight=weight, out=out)
-    _expect("k", k, (*rows, N, D), q.dtype)
-    _expect("v", v, (*rows, N, D), q.dtype)
-    _expect("lens", lens, rows, torch.int32)
-    _expect("weight", weight, (*rows, N), torch.float32)
-    _expect("out", out, q.shape, q.dtype)
+    shape, dt, device = q.shape, q.dtype, ctx.device
+    rows, (group, T, D), N = shape[:-3], shape[-3:], k.shape[-2]
+    cache = rows + (N, D)
     if out is None:
-        out = torch.empty_like(q, memory_format=torch.contiguous_format)
-    _check(load().proxykv_attend(ctx.handle, _dev_ptr(q, "q"), _dev_ptr(k, "k"), _dev_ptr(v, "v"), _dev_ptr(lens, "lens"), _cache_dtype(q),
-                                 rows.numel(), N, group, T, D, _dev_ptr(out, "out"), _dev_ptr(weight, "weight"), _stream_on(ctx, stream)),
-           "proxykv_attend", ctx.handle)
+        out = torch.empty(shape, dtype=dt, device=q.device)
+    _check(load().proxykv_attend(ctx.handle, _arg("q", q, device, dt, shape), _arg("k", k, device, dt, cache), _arg("v", v, device, dt, cache),
+                                 _arg("lens", lens, device, torch.int32, rows), _cache_dtype(q), rows.numel(), N, group, T, D,
+                                 _arg("out", out, device, dt, shape), _arg("weight", weight, device, torch.float32, rows + (N,)),
+                                 _stream_on(device, stream)), "proxykv_attend", ctx.handle)
     return out
 
 
@@ -404,51 +407,37 @@ def proxykv_attend_shared(ctx: Context, q, k_shared, v_shared, k=None, v=None, s
     """The same for a batch that shares a long context: q [batch, heads, group, T, D], k_shared and v_shared [heads, P, D] with shared_lens
     int32 [heads], k and v [batch, heads, N, D] (None: no tokens of their own) with lens int32 [batch, heads]; weight_shared fp32 [heads, P] and
     weight fp32 [batch, heads, N], if given, are added every token's probabilities."""
-    batch, heads, group, T, D = q.shape
-    P = k_shared.shape[-2]
     if (k is None) != (v is None):
         raise ValueError("k and v go together")
     if k is None and not (lens is None and weight is None):
         raise ValueError("lens and weight are those of own tokens, k and v")
-    N = 0 if k is None else k.shape[-2]
-    _on_device(ctx, q=q, k_shared=k_shared, v_shared=v_shared, k=k, v=v, shared_lens=shared_lens, lens=lens, weight_shared=weight_shared,
-               weight=weight, out=out)
-    for name, t in (("k_shared", k_shared), ("v_shared", v_shared)):
-        _expect(name, t, (heads, P, D), q.dtype)
-    for name, t in (("k", k), ("v", v)):
-        _expect(name, t, (batch, heads, N, D), q.dtype)
-    _expect("shared_lens", shared_lens, (heads,), torch.int32)
-    _expect("lens", lens, (batch, heads), torch.int32)
-    _expect("weight_shared", weight_shared, (heads, P), torch.float32)
-    _expect("weight", weight, (batch, heads, N), torch.float32)
-    _expect("out", out, q.shape, q.dtype)
+    shape, dt, device = q.shape, q.dtype, ctx.device
+    batch, heads, group, T, D = shape
+    P, N = k_shared.shape[-2], 0 if k is None else k.shape[-2]
+    both, own = (heads, P, D), (batch, heads, N, D)
     if out is None:
-        out = torch.empty_like(q, memory_format=torch.contiguous_format)
-    own = N > 0
-    _check(load().proxykv_attend_shared(ctx.handle, _dev_ptr(q, "q"), _dev_ptr(k_shared, "k_shared"), _dev_ptr(v_shared, "v_shared"),
-                                        _dev_ptr(shared_lens, "shared_lens"), _dev_ptr(k, "k") if own else None, _dev_ptr(v, "v") if own else None,
-                                        _dev_ptr(lens, "lens"), _cache_dtype(q), batch, heads, P, N, group, T, D, _dev_ptr(out, "out"),
-                                        _dev_ptr(weight_shared, "weight_shared"), _dev_ptr(weight, "weight") if own else None,
-                                        _stream_on(ctx, stream)), "proxykv_attend_shared", ctx.handle)
+        out = torch.empty(shape, dtype=dt, device=q.device)
+    args = [_arg("q", q, device, dt, shape), _arg("k_shared", k_shared, device, dt, both), _arg("v_shared", v_shared, device, dt, both),
+            _arg("shared_lens", shared_lens, device, torch.int32, (heads,)), _arg("k", k, device, dt, own), _arg("v", v, device, dt, own),
+            _arg("lens", lens, device, torch.int32, (batch, heads))]
+    weights = [_arg("weight_shared", weight_shared, device, torch.float32, (heads, P)), _arg("weight", weight, device, torch.float32, own[:3])]
+    _check(load().proxykv_attend_shared(ctx.handle, *args, _cache_dtype(q), batch, heads, P, N, group, T, D, _arg("out", out, device, dt, shape),
+                                        *weights, _stream_on(device, stream)), "proxykv_attend_shared", ctx.handle)
     return out
 
 
 def proxykv_evict(ctx: Context, k, v, weight, lens, budget, recent: int, positions=None, stream=None) -> None:
     """Rows of k, v [..., N, D], weight fp32 [..., N], positions int32 [..., N] (or None) and lens int32 [...] that hold more than `budget` tokens
     are cut to it where they lie: the `recent` last tokens and the heaviest others stay.  budget: an int, or an int32 tensor [...]."""
-    N, D, rows = k.shape[-2], k.shape[-1], k.shape[:-2]
-    budgets = budget if isinstance(budget, torch.Tensor) else None
-    _on_device(ctx, k=k, v=v, weight=weight, lens=lens, positions=positions, budget=budgets)
+    shape, dt, device = k.shape, k.dtype, ctx.device
+    rows, row, (N, D) = shape[:-2], shape[:-1], shape[-2:]
     if k.element_size() != 2:
         raise ValueError("k and v must have 16-bit elements")
-    _expect("v", v, k.shape, k.dtype)
-    _expect("weight", weight, (*rows, N), torch.float32)
-    _expect("lens", lens, rows, torch.int32)
-    _expect("positions", positions, (*rows, N), torch.int32)
-    _expect("budget", budgets, rows, torch.int32)
-    _check(load().proxykv_evict(ctx.handle, _dev_ptr(k, "k"), _dev_ptr(v, "v"), _dev_ptr(weight, "weight"), _dev_ptr(positions, "positions"),
-                                _dev_ptr(lens, "lens"), _dev_ptr(budgets, "budget"), rows.numel(), N, 0 if budgets is not None else int(budget),
-                                recent, D, _stream_on(ctx, stream)), "proxykv_evict", ctx.handle)
+    own = isinstance(budget, torch.Tensor)
+    _check(load().proxykv_evict(ctx.handle, _arg("k", k, device, dt, shape), _arg("v", v, device, dt, shape),
+                                _arg("weight", weight, device, torch.float32, row), _arg("positions", positions, device, torch.int32, row),
+                                _arg("lens", lens, device, torch.int32, rows), _arg("budget", budget, device, torch.int32, rows) if own else None,
+                                rows.numel(), N, 0 if own else int(budget), recent, D, _stream_on(device, stream)), "proxykv_evict", ctx.handle)
 
 
 def proxykv_prune(ctx: Context, q_rec, k_ctx, k_rec, chunk: int, keep_ratio: float, k_in, v_in, k_out=None, v_out=None,

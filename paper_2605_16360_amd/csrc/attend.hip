@@ -360,78 +360,131 @@ __global__ __launch_bounds__(64 * W, W < 4 ? 1 : W / 4) void attend_block_kernel
   Part<D, F16, 2, W>::run(a, p, ks, shared, row, split, tile, lds);
 }
 
-// (m, l) of a query's shares joined, by a wave: 2^m l is the sum of all
+// A query's shares, or some of them, put together: 2^m l is their sum, 2^m o their output.
 struct Joined {
   float m, l;
 };
-__device__ __forceinline__ Joined join(const float* ml, int64_t query, int64_t queries, int splits, int lane) {
+__device__ __forceinline__ Joined join(const float* ml, int64_t query, int64_t queries, int splits, int lane) {  // by a wave
   float m = kLow, l = 0.0f;
-  for (int s0 = 0; s0 < splits; s0 += 64) {
-    const int s = s0 + lane;
-    const float2 x = s < splits ? reinterpret_cast<const float2*>(ml)[(size_t)s * queries + query] : float2{kLow, 0.0f};
-    float top = x.x;
-    for (int off = 32; off; off >>= 1) top = __builtin_fmaxf(top, __shfl_xor(top, off, 64));
-    top = __builtin_fmaxf(m, top);
-    float sum = x.y * __builtin_amdgcn_exp2f(x.x - top);
-    for (int off = 32; off; off >>= 1) sum += __shfl_xor(sum, off, 64);
-    l = l * __builtin_amdgcn_exp2f(m - top) + sum;
+  for (int s = lane; s < splits; s += 64) {
+    const float2 x = reinterpret_cast<const float2*>(ml)[(size_t)s * queries + query];
+    const float top = __builtin_fmaxf(m, x.x);
+    l = l * __builtin_amdgcn_exp2f(m - top) + x.y * __builtin_amdgcn_exp2f(x.x - top);
+    m = top;
+  }
+  for (int off = 32; off; off >>= 1) {
+    const float m2 = __shfl_xor(m, off, 64), l2 = __shfl_xor(l, off, 64), top = __builtin_fmaxf(m, m2);
+    l = l * __builtin_amdgcn_exp2f(m - top) + l2 * __builtin_amdgcn_exp2f(m2 - top);
     m = top;
   }
   return {m, l};
 }
 
-// Blocks below `query_blocks`: four queries each, a wave for one: the shares' outputs joined.  The others: the account of 1024 keys of a row.
-template <int D, bool F16>
-__global__ __launch_bounds__(256) void attend_finish_kernel(AttendArgs a, Plan p, int query_blocks, int shared_blocks) {
-  __shared__ float lse[kKeptQueries];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, per = (int)(a.group * a.T);
-  if ((int)blockIdx.x < query_blocks) {
-    const int64_t query = (int64_t)blockIdx.x * 4 + wave;
-    if (query >= p.queries) return;
-    const Joined j = join(p.ml, query, p.queries, p.splits, lane);
-    float x[D / 64] = {};
-    for (int s = 0; s < p.splits; ++s) {
-      const float2 ml = reinterpret_cast<const float2*>(p.ml)[(size_t)s * p.queries + query];
-      const float f = __builtin_amdgcn_exp2f(ml.x - j.m);
-      if (ml.y != 0.0f) {
-        const float* o = p.o + ((size_t)s * p.queries + query) * D + lane * (D / 64);
+// Joins the shares' outputs: D / 4 threads hold a share's row, so that a block takes 4 queries of few shares (QB = 4), or one query's
+// 256 / (D / 4) shares at a time.
+template <int D, bool F16, int QB>
+__device__ __forceinline__ void join_outputs(const AttendArgs& a, const Plan& p, int block) {
+  constexpr int LPR = D / 4, G = 256 / LPR / QB;  // threads per row; shares at a time
+  __shared__ float part[256 / LPR][D];
+  __shared__ float2 part_ml[256 / LPR];
+  const int tid = threadIdx.x, g = tid / LPR, at = tid % LPR * 4, per = (int)(a.group * a.T);
+  const int64_t mine = (int64_t)block * QB + g / G, query = mine < p.queries ? mine : p.queries - 1;
+  float m = kLow, l = 0.0f;
+  f32x4 x = {0, 0, 0, 0};
+  constexpr int U = 4;
+  for (int s0 = g % G; s0 < p.splits; s0 += G * U) {
+    float2 ml[U];
+    f32x4 o[U];
 #pragma unroll
-        for (int e = 0; e < D / 64; ++e) x[e] = __builtin_fmaf(f, o[e], x[e]);
-      }
+    for (int u = 0; u < U; ++u) {  // (a share behind the last reads that one and counts nothing; one without keys has left no output)
+      const int s = s0 + u * G < p.splits ? s0 + u * G : p.splits - 1;
+      ml[u] = reinterpret_cast<const float2*>(p.ml)[(size_t)s * p.queries + query];
+      o[u] = *reinterpret_cast<const f32x4*>(p.o + ((size_t)s * p.queries + query) * D + at);
     }
-    const bool none = j.l == 0.0f;
 #pragma unroll
-    for (int e = 0; e < D / 64; ++e) ((uint16_t*)a.out)[query * D + lane * (D / 64) + e] = Elem<F16>::narrow(none ? 0.0f : x[e] / j.l);
-    if (lane == 0 && p.lse != nullptr) {
-      const float v = none ? -kNegInf : j.m + __builtin_amdgcn_logf(j.l);
-      p.lse[query] = v;
-      const int64_t row = query / per;  // (sequence, head)
-      p.lse[p.queries + (row % a.heads * a.batch + row / a.heads) * per + query % per] = v;
+    for (int u = 0; u < U; ++u) {
+      if (s0 + u * G >= p.splits || ml[u].y == 0.0f) continue;
+      const float top = __builtin_fmaxf(m, ml[u].x), f = __builtin_amdgcn_exp2f(m - top), f2 = __builtin_amdgcn_exp2f(ml[u].x - top);
+      l = l * f + ml[u].y * f2;
+      x = x * f + o[u] * f2;
+      m = top;
     }
-    return;
   }
-  int b = blockIdx.x - query_blocks;
-  const bool shared = b < shared_blocks;
-  if (!shared) b -= shared_blocks;
-  const Keys& ks = shared ? p.shared : p.own;
-  const int blocks = (int)((ks.n + 1023) / 1024), n0 = b % blocks * 1024, M = (int)ks.m, T = (int)a.T;
+  if constexpr (G > 1) {
+    *reinterpret_cast<f32x4*>(&part[g][at]) = x;
+    if (at == 0) part_ml[g] = float2{m, l};
+    __syncthreads();
+    if (g % G != 0) return;
+    for (int i = 1; i < G; ++i) {
+      const float2 ml = part_ml[g + i];
+      const float top = __builtin_fmaxf(m, ml.x), f = __builtin_amdgcn_exp2f(m - top), f2 = __builtin_amdgcn_exp2f(ml.x - top);
+      l = l * f + ml.y * f2;
+      x = x * f + *reinterpret_cast<const f32x4*>(&part[g + i][at]) * f2;
+      m = top;
+    }
+  }
+  if (mine >= p.queries) return;
+  const bool none = l == 0.0f;
+  u32x2 r = {0, 0};
+  if (!none) {
+    const f32x4 y = x / l;
+    r = u32x2{Elem<F16>::narrow(y[0]) | (uint32_t)Elem<F16>::narrow(y[1]) << 16, Elem<F16>::narrow(y[2]) | (uint32_t)Elem<F16>::narrow(y[3]) << 16};
+  }
+  *reinterpret_cast<u32x2*>((uint16_t*)a.out + query * D + at) = r;
+  if (at == 0 && p.lse != nullptr) {
+    const float v = none ? -kNegInf : m + __builtin_amdgcn_logf(l);
+    p.lse[query] = v;
+    const int64_t row = query / per;  // (sequence, head)
+    p.lse[p.queries + (row % a.heads * a.batch + row / a.heads) * per + query % per] = v;
+  }
+}
+
+// The account of 1024 keys of a row from logits that were kept, of up to MQ queries.
+template <int D, int MQ>
+__device__ __forceinline__ void account_kept(const AttendArgs& a, const Plan& p, const Keys& ks, bool shared, int b) {
+  __shared__ float lse[MQ];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, per = (int)(a.group * a.T), M = (int)ks.m, T = (int)a.T;
+  const int blocks = (int)((ks.n + 1023) / 1024), n = b % blocks * 1024 + threadIdx.x * 4;
   const int64_t row = b / blocks;
   const int len = row_len(shared ? a.shared_lens : a.lens, row, ks.n);
-  if (n0 >= len) return;
+  if (b % blocks * 1024 >= len) return;
+  // (asked for before the joins: score rows have room for a whole quad)
+  const bool any = n < len;
+  f32x4 s[MQ];
+#pragma unroll
+  for (int m = 0; m < MQ; ++m)
+    s[m] = *reinterpret_cast<const f32x4*>(ks.scores + ((size_t)row * M + (m < M ? m : M - 1)) * ks.score_stride + (any ? n : 0));
+  float* w = (shared ? a.weight_shared : a.weight) + row * ks.n;
+  f32x4 x;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) x[e] = w[n + e < len ? n + e : len - 1];
   for (int m = wave; m < M; m += 4) {
     const Joined j = join(p.ml, query_at(shared, row, m, per, a.heads), p.queries, p.splits, lane);
     if (lane == 0) lse[m] = j.l == 0.0f ? -kNegInf : j.m + __builtin_amdgcn_logf(j.l);
   }
   __syncthreads();
   const float c = kLog2e / __builtin_sqrtf((float)D);
-  float* w = (shared ? a.weight_shared : a.weight) + row * ks.n;
-  for (int n = n0 + threadIdx.x; n < n0 + 1024 && n < len; n += 256) {
-    float sum = 0.0f;
-    for (int m = 0; m < M; ++m) {
-      const float s = ks.scores[((size_t)row * M + m) * ks.score_stride + n];
-      sum += shared || n < seen(len, T, m % T) ? __builtin_amdgcn_exp2f(__builtin_fmaf(s, c, -lse[m])) : 0.0f;
-    }
-    w[n] += sum;
+  f32x4 sum = {0, 0, 0, 0};
+#pragma unroll
+  for (int m = 0; m < MQ; ++m) {
+    const float ref = m < M ? lse[m] : -kNegInf;
+    const int see = m < M ? shared ? len : seen(len, T, m % T) : 0;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) sum[e] += n + e < see ? __builtin_amdgcn_exp2f(__builtin_fmaf(s[m][e], c, -ref)) : 0.0f;
+  }
+#pragma unroll
+  for (int e = 0; e < 4; ++e)
+    if (n + e < len) w[n + e] = x[e] + sum[e];
+}
+
+// Blocks below `query_blocks` join outputs, those behind them keep the account.
+template <int D, bool F16, int QB, int MQ>
+__global__ __launch_bounds__(256) void attend_finish_kernel(AttendArgs a, Plan p, int query_blocks, int shared_blocks) {
+  const int b = (int)blockIdx.x - query_blocks;
+  if (b < 0) return join_outputs<D, F16, QB>(a, p, blockIdx.x);
+  if constexpr (MQ > 0) {
+    const bool shared = b < shared_blocks;
+    account_kept<D, MQ>(a, p, shared ? p.shared : p.own, shared, shared ? b : b - shared_blocks);
   }
 }
 
@@ -490,7 +543,13 @@ __global__ __launch_bounds__(256) void attend_account_kernel(AttendArgs a, Keys 
 }
 
 // Shares of at least kLeastKeys keys, as many as give the chip kWaves waves of this kind.
-constexpr int64_t kLeastKeys = 256, kWaves = 2048;
+#ifndef PKV_LEAST
+#define PKV_LEAST 128
+#endif
+#ifndef PKV_WAVES
+#define PKV_WAVES 2048
+#endif
+constexpr int64_t kLeastKeys = PKV_LEAST, kWaves = PKV_WAVES, kMostSplits = 512;
 
 Keys keys_of(int64_t rows, int64_t n, int64_t m, bool account) {
   Keys k = {};
@@ -508,6 +567,7 @@ Keys keys_of(int64_t rows, int64_t n, int64_t m, bool account) {
   int64_t splits = (kWaves + rows * k.tiles * k.waves - 1) / (rows * k.tiles * k.waves);
   const int64_t most = (n + kLeastKeys - 1) / kLeastKeys;
   splits = splits < most ? splits : most;
+  splits = splits < kMostSplits ? splits : kMostSplits;
   k.chunk = (int)(((n + splits - 1) / splits + kTile - 1) / kTile * kTile);
   k.splits = (int)((n + k.chunk - 1) / k.chunk);
   k.blocks = (int)((rows * k.splits + kXcds - 1) / kXcds * kXcds * k.tiles);
@@ -562,10 +622,22 @@ hipError_t launch_attend_of(const AttendArgs& a, void* scratch, hipStream_t stre
     e = hipGetLastError();
   }
   if (e != hipSuccess) return e;
-  const int query_blocks = (int)((p.queries + 3) / 4);
   const int64_t shared_blocks = p.shared.scores ? p.shared.rows * ((p.shared.n + 1023) / 1024) : 0;
   const int64_t own_blocks = p.own.scores ? p.own.rows * ((p.own.n + 1023) / 1024) : 0;
-  attend_finish_kernel<D, F16><<<(unsigned)(query_blocks + shared_blocks + own_blocks), 256, 0, stream>>>(a, p, query_blocks, (int)shared_blocks);
+  const int64_t kept_shared = p.shared.scores ? p.shared.m : 0, kept_own = p.own.scores ? p.own.m : 0, kept = kept_shared > kept_own ? kept_shared : kept_own;
+  auto finish = [&](auto qb, auto mq) {
+    constexpr int QB = decltype(qb)::value, MQ = decltype(mq)::value;
+    const int query_blocks = (int)((p.queries + QB - 1) / QB);
+    attend_finish_kernel<D, F16, QB, MQ><<<(unsigned)(query_blocks + shared_blocks + own_blocks), 256, 0, stream>>>(a, p, query_blocks, (int)shared_blocks);
+  };
+  auto finish_of = [&](auto qb) {
+    if (kept == 0) finish(qb, std::integral_constant<int, 0>{});
+    else if (kept <= 4) finish(qb, std::integral_constant<int, 4>{});
+    else if (kept <= 8) finish(qb, std::integral_constant<int, 8>{});
+    else finish(qb, std::integral_constant<int, 16>{});
+  };
+  if (p.splits <= 8) finish_of(std::integral_constant<int, 4>{});
+  else finish_of(std::integral_constant<int, 1>{});
   e = hipGetLastError();
   if (e == hipSuccess && a.weight_shared != nullptr && !p.shared.scores) {
     attend_account_kernel<D, F16><<<(unsigned)(p.shared.rows * ((p.shared.n + 255) / 256)), 256, 0, stream>>>(a, p.shared, true, p.lse + p.queries);

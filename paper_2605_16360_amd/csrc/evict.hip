@@ -10,7 +10,8 @@ namespace pkv {
 namespace {
 
 constexpr int kSelThreads = 1024, kSelWaves = kSelThreads / 64;
-constexpr int kPlanHead = 4;  // words: moves, candidates, keep, recent tokens to move up (0: nothing to do)
+constexpr int kBins = 2048, kCopies = 8;  // of a digit's histogram: accounts share their high digits, and lanes that meet in a word take turns
+constexpr int kPlanHead = 4;              // words: moves, candidates, keep, recent tokens to move up (0: nothing to do)
 
 // Larger key <=> heavier.  NaN maps to 0 (below every number), -0.0 onto +0.0.
 __device__ __forceinline__ uint32_t weight_key(float f) {
@@ -19,14 +20,17 @@ __device__ __forceinline__ uint32_t weight_key(float f) {
   return f == f ? k : 0u;
 }
 
-// One workgroup per row: the keep-th heaviest candidate by a radix select of four digits, the lists of moves in order, then the moves of
-// the account and the positions themselves.
+// One workgroup per row: the keep-th heaviest candidate by a radix select of 11, 11 and 10 bits, the lists of moves in order, then the moves
+// of the account and the positions themselves.  A wave has consecutive candidates, 64 at a time, so that ranks need one exchange
+// between waves.  STEPS > 0: a lane keeps its candidates' keys, STEPS of them, in registers; 0: they are read again for each use.
+template <int STEPS>
 __global__ __launch_bounds__(kSelThreads) void evict_select_kernel(float* __restrict__ weight, int32_t* __restrict__ positions,
                                                                    int32_t* __restrict__ lens, const int32_t* __restrict__ budgets, int64_t N,
                                                                    int budget, int recent, int32_t* __restrict__ plans, int64_t plan_words) {
-  __shared__ uint32_t hist[256];
-  __shared__ int s_eq[kSelWaves], s_list[kSelWaves];
+  __shared__ u32x4 hist4[kBins * kCopies / 4];
+  __shared__ int s_wave[2][kSelWaves];
   __shared__ uint32_t s_prefix, s_left;
+  uint32_t* hist = reinterpret_cast<uint32_t*>(hist4);
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int64_t r = blockIdx.x;
   int32_t* plan = plans + r * plan_words;
@@ -46,68 +50,112 @@ __global__ __launch_bounds__(kSelThreads) void evict_select_kernel(float* __rest
   const int cand = n - recent, keep = b - recent;
   int moves = 0;
   if (keep > 0) {
-    uint32_t prefix = 0, left = (uint32_t)keep;
-    for (int shift = 24; shift >= 0; shift -= 8) {
-      if (tid < 256) hist[tid] = 0;
-      __syncthreads();
-      for (int i = tid; i < cand; i += kSelThreads) {
-        const uint32_t k = weight_key(w[i]);
-        if (shift == 24 || (k >> (shift + 8)) == (prefix >> (shift + 8))) atomicAdd(&hist[(k >> shift) & 255u], 1u);
-      }
-      __syncthreads();
-      if (wave == 0) {  // lane l has bins 255 - 4 l downwards
-        uint32_t h[4], sum = 0;
-        for (int e = 0; e < 4; ++e) sum += h[e] = hist[255 - 4 * lane - e];
-        uint32_t upto = sum;
-        for (int off = 1; off < 64; off *= 2) {
-          const uint32_t o = __shfl_up(upto, off, 64);
-          upto += lane >= off ? o : 0u;
+    const int steps = STEPS > 0 ? STEPS : (cand + kSelThreads - 1) / kSelThreads, first = wave * steps * 64 + lane;
+    uint32_t keys[STEPS > 0 ? STEPS : 1];
+    if constexpr (STEPS > 0) {  // (no branch around a load; what lies behind the last candidate counts nowhere)
+#pragma unroll
+      for (int j = 0; j < STEPS; ++j) keys[j] = __float_as_uint(w[first + j * 64 < cand ? first + j * 64 : cand - 1]);
+#pragma unroll
+      for (int j = 0; j < STEPS; ++j) keys[j] = weight_key(__uint_as_float(keys[j]));
+    }
+    // f(place, key) for this lane's places, in order; a place behind the last candidate has place >= cand
+    auto each = [&](auto f) __attribute__((always_inline)) {
+      if constexpr (STEPS > 0) {
+#pragma unroll
+        for (int j = 0; j < STEPS; ++j) f(first + j * 64, keys[j]);
+      } else {
+        constexpr int U = 8;
+        for (int j0 = 0; j0 < steps; j0 += U) {
+          float x[U];
+#pragma unroll
+          for (int u = 0; u < U; ++u) x[u] = w[first + (j0 + u) * 64 < cand ? first + (j0 + u) * 64 : cand - 1];
+#pragma unroll
+          for (int u = 0; u < U; ++u)
+            if (j0 + u < steps) f(first + (j0 + u) * 64, weight_key(x[u]));
         }
-        uint32_t above = upto - sum;
-        if (above < left && upto >= left)
-          for (int e = 0; e < 4; ++e) {
-            if (above < left && above + h[e] >= left) {
-              s_prefix = prefix | (uint32_t)(255 - 4 * lane - e) << shift;
-              s_left = left - above;
-            }
-            above += h[e];
-          }
+      }
+    };
+    uint32_t prefix = 0, left = (uint32_t)keep;
+    static_for<3>([&](auto digit) __attribute__((always_inline)) {
+      constexpr int shift = decltype(digit)::value == 0 ? 21 : decltype(digit)::value == 1 ? 10 : 0, bits = decltype(digit)::value == 2 ? 10 : 11;
+#pragma unroll
+      for (int i = 0; i < kBins * kCopies / 4 / kSelThreads; ++i) hist4[i * kSelThreads + tid] = u32x4{0, 0, 0, 0};
+      __syncthreads();
+      each([&](int i, uint32_t k) __attribute__((always_inline)) {
+        if (i < cand && (shift == 21 || (k >> (shift + bits < 32 ? shift + bits : 31)) == (prefix >> (shift + bits < 32 ? shift + bits : 31))))
+          atomicAdd(&hist[((k >> shift) & ((1u << bits) - 1u)) * kCopies + (lane & (kCopies - 1))], 1u);
+      });
+      __syncthreads();
+      // thread t has the bins 2047 - 2 t and 2046 - 2 t: how many keys lie above them, from the highest downwards
+      uint32_t h[2];
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        const u32x4 x = hist4[(kBins - 1 - 2 * tid - e) * 2], y = hist4[(kBins - 1 - 2 * tid - e) * 2 + 1];
+        h[e] = x[0] + x[1] + x[2] + x[3] + y[0] + y[1] + y[2] + y[3];
+      }
+      uint32_t upto = h[0] + h[1];
+      for (int off = 1; off < 64; off *= 2) {
+        const uint32_t o = __shfl_up(upto, off, 64);
+        upto += lane >= off ? o : 0u;
+      }
+      if (lane == 63) s_wave[0][wave] = (int)upto;
+      __syncthreads();
+      for (int x = 0; x < kSelWaves; ++x) upto += x < wave ? (uint32_t)s_wave[0][x] : 0u;
+      uint32_t above = upto - h[0] - h[1];
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        if (above < left && above + h[e] >= left) {
+          s_prefix = prefix | (uint32_t)(kBins - 1 - 2 * tid - e) << shift;
+          s_left = left - above;
+        }
+        above += h[e];
       }
       __syncthreads();
       prefix = s_prefix;
       left = s_left;
-    }
+    });
     // kept: above the key, or equal to it and among the first `left` of those
-    uint32_t equal = 0;
-    int holes = 0;
-    for (int i0 = 0; i0 < cand; i0 += kSelThreads) {
-      const int i = i0 + tid;
-      const uint32_t k = i < cand ? weight_key(w[i]) : 0u;
-      const bool eq = i < cand && k == prefix;
-      const uint64_t eq_mask = __builtin_amdgcn_ballot_w64(eq), below = (1ull << lane) - 1;
-      if (lane == 0) s_eq[wave] = __popcll(eq_mask);
-      __syncthreads();
-      uint32_t rank = equal + __popcll(eq_mask & below);
-      for (int x = 0; x < kSelWaves; ++x) {
-        rank += x < wave ? s_eq[x] : 0;
-        equal += s_eq[x];
-      }
-      const bool kept = i < cand && (k > prefix || (eq && rank < left));
-      const bool hole = i < keep && !kept, filler = i >= keep && kept;
-      const uint64_t hole_mask = __builtin_amdgcn_ballot_w64(hole), fill_mask = __builtin_amdgcn_ballot_w64(filler);
-      if (lane == 0) s_list[wave] = __popcll(hole_mask) | __popcll(fill_mask) << 16;
-      __syncthreads();
-      int h = holes + __popcll(hole_mask & below), f = moves + __popcll(fill_mask & below);
-      for (int x = 0; x < kSelWaves; ++x) {
-        const int c = s_list[x];
-        h += x < wave ? c & 0xffff : 0;
-        f += x < wave ? c >> 16 : 0;
-        holes += c & 0xffff;
-        moves += c >> 16;
-      }
-      if (hole) to[h] = i;
-      if (filler) from[f] = i;
+    const uint64_t below = (1ull << lane) - 1;
+    int equal = 0;
+    each([&](int i, uint32_t k) __attribute__((always_inline)) { equal += __popcll(__builtin_amdgcn_ballot_w64(i < cand && k == prefix)); });
+    if (lane == 0) s_wave[1][wave] = equal;
+    __syncthreads();
+    int before = 0;
+    for (int x = 0; x < kSelWaves; ++x) before += x < wave ? s_wave[1][x] : 0;
+    // f(place, whether it is given up among the first `keep` places, whether it is kept behind them, this lane's masks of both)
+    auto marks = [&](auto f) __attribute__((always_inline)) {
+      int rank0 = before;
+      each([&](int i, uint32_t k) __attribute__((always_inline)) {
+        const uint64_t eq = __builtin_amdgcn_ballot_w64(i < cand && k == prefix);
+        const bool kept = i < cand && (k > prefix || (k == prefix && rank0 + __popcll(eq & below) < (int)left));
+        rank0 += __popcll(eq);
+        const bool hole = i < keep && !kept, filler = i >= keep && kept;
+        f(i, hole, filler, __builtin_amdgcn_ballot_w64(hole), __builtin_amdgcn_ballot_w64(filler));
+      });
+    };
+    int holes = 0, fillers = 0;
+    marks([&](int, bool, bool, uint64_t h, uint64_t f) __attribute__((always_inline)) {
+      holes += __popcll(h);
+      fillers += __popcll(f);
+    });
+    __syncthreads();
+    if (lane == 0) {
+      s_wave[0][wave] = holes;
+      s_wave[1][wave] = fillers;
     }
+    __syncthreads();
+    holes = fillers = 0;
+    for (int x = 0; x < kSelWaves; ++x) {
+      holes += x < wave ? s_wave[0][x] : 0;
+      fillers += x < wave ? s_wave[1][x] : 0;
+      moves += s_wave[1][x];
+    }
+    marks([&](int i, bool hole, bool filler, uint64_t h, uint64_t f) __attribute__((always_inline)) {
+      if (hole) to[holes + __popcll(h & below)] = i;
+      if (filler) from[fillers + __popcll(f & below)] = i;
+      holes += __popcll(h);
+      fillers += __popcll(f);
+    });
     __syncthreads();
   }
   if (tid == 0) {
@@ -118,8 +166,9 @@ __global__ __launch_bounds__(kSelThreads) void evict_select_kernel(float* __rest
   }
   int32_t* pos = positions == nullptr ? nullptr : positions + r * N;
   for (int j = tid; j < moves; j += kSelThreads) {
-    w[to[j]] = w[from[j]];
-    if (pos != nullptr) pos[to[j]] = pos[from[j]];
+    const int x = from[j], y = to[j];
+    w[y] = w[x];
+    if (pos != nullptr) pos[y] = pos[x];
   }
   __syncthreads();
   // a recent token never moves back, so what a step stores is behind nothing that a later one reads
@@ -141,47 +190,81 @@ __global__ __launch_bounds__(kSelThreads) void evict_select_kernel(float* __rest
   if (tid == 0) lens[r] = b;
 }
 
-// The planned moves of K and V.  K and V, and the slices of a token, are independent, so each gets a workgroup.  First the candidates, whose new
-// places nothing else reads; their old places may be the recent tokens' new ones, so every one of them has been read before those are stored.
-// grid (rows, 2 * slices), 256 threads; cpr = 16-byte pieces per token, cps = those of a slice.
-template <int PER>
+// The planned moves of K and V.  K and V, and the slices of a token, are independent, so each gets workgroups of its own.  A candidate's new
+// place is nothing that is read any more, but the recent tokens' new places, keep .. b - 1, are the old places of the first moves.  Those
+// and the recent tokens are one list, which one workgroup walks in order, a step's loads under way while the one before is stored:
+// what a step stores lies on nothing that a later step reads (a recent token's new place is the old one of an earlier entry), so each
+// waits only for its own loads, in all threads, before it stores.  Moves from behind the budget are anybody's: blockIdx.z > 0, free_tokens each.
+// grid (rows, 2 * slices, 1 + blocks for the free moves), 256 threads; cpr = 16-byte pieces per token, cps those of a slice.
+constexpr int kPer = 4;
 __global__ __launch_bounds__(256) void evict_move_kernel(u32x4* __restrict__ k, u32x4* __restrict__ v, const int32_t* __restrict__ plans,
-                                                         int64_t plan_words, int64_t N, int cpr, int cps) {
+                                                         int64_t plan_words, int64_t N, int cpr, int cps, int free_tokens) {
   const int64_t r = blockIdx.x;
-  const int tid = threadIdx.x;
+  const int tid = threadIdx.x, step = 256 * kPer / cps;  // tokens at a time
   const int32_t* plan = plans + r * plan_words;
-  const int moves = plan[0], cand = plan[1], keep = plan[2], recent = plan[3];
+  const int moves = plan[0], cand = plan[1], keep = plan[2], recent = plan[3], b = keep + recent;
   const int32_t *from = plan + kPlanHead, *to = from + (plan_words - kPlanHead) / 2;
-  u32x4* base = ((blockIdx.y & 1) ? v : k) + (size_t)r * N * cpr + (blockIdx.y >> 1) * cps;
-  for (int64_t i0 = 0; i0 < (int64_t)moves * cps; i0 += 256 * PER) {
-    u32x4 x[PER];
-#pragma unroll
-    for (int u = 0; u < PER; ++u) {
-      const int64_t i = i0 + u * 256 + tid;
-      if (i < (int64_t)moves * cps) x[u] = base[(size_t)from[i / cps] * cpr + i % cps];
+  int bound = 0;  // moves from in front of the budget's end: those come first
+  for (int lo = 0, hi = moves;;) {
+    if (lo >= hi) {
+      bound = lo;
+      break;
     }
-#pragma unroll
-    for (int u = 0; u < PER; ++u) {
-      const int64_t i = i0 + u * 256 + tid;
-      if (i < (int64_t)moves * cps) base[(size_t)to[i / cps] * cpr + i % cps] = x[u];
-    }
+    const int mid = (lo + hi) / 2;
+    if (from[mid] < b) lo = mid + 1;
+    else hi = mid;
   }
-  __syncthreads();
-  for (int64_t i0 = 0; i0 < (int64_t)recent * cps; i0 += 256 * PER) {
-    u32x4 x[PER] = {};
+  u32x4* base = ((blockIdx.y & 1) ? v : k) + (size_t)r * N * cpr + (blockIdx.y >> 1) * cps;
+  const bool free = blockIdx.z > 0;
+  const int64_t begin64 = free ? bound + ((int64_t)blockIdx.z - 1) * free_tokens : 0;
+  const int64_t end64 = free ? (begin64 + free_tokens < moves ? begin64 + free_tokens : moves) : (int64_t)bound + recent;
+  if (begin64 >= end64) return;
+  const int begin = (int)begin64, end = (int)end64;
+  auto places = [&](int j, int& src, int& dst) __attribute__((always_inline)) {  // of entry j; the free moves have no recent tokens
+    const int jm = j < moves ? j : moves > 0 ? moves - 1 : 0;
+    const bool move = free || j < bound;
+    const int x = from[jm], y = to[jm];
+    src = move ? x : cand + j - bound;
+    dst = move ? y : keep + j - bound;
+  };
+  int tok[kPer], ch[kPer];
 #pragma unroll
-    for (int u = 0; u < PER; ++u) {
-      const int64_t i = i0 + u * 256 + tid;
-      if (i < (int64_t)recent * cps) x[u] = base[(size_t)(cand + i / cps) * cpr + i % cps];
+  for (int u = 0; u < kPer; ++u) {
+    const int piece = tid + 256 * u;
+    tok[u] = piece < step * cps ? piece / cps : 1 << 30;
+    ch[u] = piece % cps;
+  }
+  auto load = [&](int j0, u32x4 (&x)[kPer], int (&dst)[kPer]) __attribute__((always_inline)) {  // (a piece behind the end reads the last token's and stores nothing)
+    int src[kPer];
+#pragma unroll
+    for (int u = 0; u < kPer; ++u) {
+      const int j = tok[u] < end - j0 ? j0 + tok[u] : end - 1;
+      places(j, src[u], dst[u]);
     }
 #pragma unroll
-    for (int u = 0; u < PER; ++u) asm volatile("" : "+v"(x[u]));  // arrived, not only asked for
+    for (int u = 0; u < kPer; ++u) x[u] = base[(size_t)src[u] * cpr + ch[u]];
+  };
+  auto store = [&](int j0, const u32x4 (&x)[kPer], const int (&dst)[kPer]) __attribute__((always_inline)) {
+#pragma unroll
+    for (int u = 0; u < kPer; ++u)
+      if (tok[u] < end - j0) base[(size_t)dst[u] * cpr + ch[u]] = x[u];
+  };
+  auto meet = [&](u32x4 (&x)[kPer]) __attribute__((always_inline)) {
+#pragma unroll
+    for (int u = 0; u < kPer; ++u) asm volatile("" : "+v"(x[u]));  // arrived, not only asked for
     __syncthreads();
-#pragma unroll
-    for (int u = 0; u < PER; ++u) {
-      const int64_t i = i0 + u * 256 + tid;
-      if (i < (int64_t)recent * cps) base[(size_t)(keep + i / cps) * cpr + i % cps] = x[u];
-    }
+  };
+  u32x4 x0[kPer], x1[kPer];
+  int d0[kPer], d1[kPer];
+  load(begin, x0, d0);
+  for (int j = begin; j < end; j += 2 * step) {  // (two steps by name: moving x1 to x0 would wait for it)
+    if (j + step < end) load(j + step, x1, d1);
+    meet(x0);
+    store(j, x0, d0);
+    if (j + step >= end) break;
+    if (j + 2 * step < end) load(j + 2 * step, x0, d0);
+    meet(x1);
+    store(j + step, x1, d1);
   }
 }
 
@@ -195,13 +278,27 @@ size_t evict_scratch_bytes(int64_t rows, int64_t N) { return (size_t)(rows * pla
 
 hipError_t launch_evict(void* k, void* v, float* weight, int32_t* positions, int32_t* lens, const int32_t* budgets, int64_t rows, int64_t N,
                         int64_t budget, int64_t recent, int64_t row_bytes, void* scratch, hipStream_t stream) {
-  const int64_t words = plan_words_of(N);
-  evict_select_kernel<<<(unsigned)rows, kSelThreads, 0, stream>>>(weight, positions, lens, budgets, N, (int)budget, (int)recent, (int32_t*)scratch, words);
+  const int64_t words = plan_words_of(N), most = N - recent;  // (candidates of a row)
+  auto select = [&](auto steps) {
+    evict_select_kernel<decltype(steps)::value><<<(unsigned)rows, kSelThreads, 0, stream>>>(weight, positions, lens, budgets, N, (int)budget, (int)recent,
+                                                                                          (int32_t*)scratch, words);
+  };
+  if (most <= 2 * kSelThreads) select(std::integral_constant<int, 2>{});
+  else if (most <= 5 * kSelThreads) select(std::integral_constant<int, 5>{});
+  else if (most <= 10 * kSelThreads) select(std::integral_constant<int, 10>{});
+  else if (most <= 20 * kSelThreads) select(std::integral_constant<int, 20>{});
+  else if (most <= 40 * kSelThreads) select(std::integral_constant<int, 40>{});
+  else select(std::integral_constant<int, 0>{});
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
   const int cpr = (int)(row_bytes / 16), slices = cpr % 8 == 0 ? cpr / 8 : 1;
-  evict_move_kernel<8><<<dim3((unsigned)rows, (unsigned)(2 * slices)), 256, 0, stream>>>((u32x4*)k, (u32x4*)v, (const int32_t*)scratch, words, N, cpr,
-                                                                                       cpr / slices);
+  // free moves of a row: kept candidates from behind the budget, no more than places in front of the recent ones, nor than candidates there
+  int64_t free = budgets != nullptr ? N / 2 : budget - recent < N - recent - budget ? budget - recent : N - recent - budget;
+  free = free > 0 ? free : 0;
+  const int64_t free_tokens = free <= 256 * 4096 ? 256 : (free + 4095) / 4096;
+  free = (free + free_tokens - 1) / free_tokens;
+  evict_move_kernel<<<dim3((unsigned)rows, (unsigned)(2 * slices), (unsigned)(1 + free)), 256, 0, stream>>>((u32x4*)k, (u32x4*)v, (const int32_t*)scratch,
+                                                                                                          words, N, cpr, cpr / slices, (int)free_tokens);
   return hipGetLastError();
 }
 
