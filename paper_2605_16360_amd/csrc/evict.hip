@@ -29,7 +29,7 @@ __global__ __launch_bounds__(kSelThreads) void evict_select_kernel(float* __rest
                                                                    int budget, int recent, int32_t* __restrict__ plans, int64_t plan_words) {
   __shared__ u32x4 hist4[kBins * kCopies / 4];
   __shared__ int s_wave[2][kSelWaves];
-  __shared__ uint32_t s_prefix, s_left;
+  __shared__ uint32_t s_prefix, s_left, s_equal;
   uint32_t* hist = reinterpret_cast<uint32_t*>(hist4);
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int64_t r = blockIdx.x;
@@ -59,20 +59,24 @@ __global__ __launch_bounds__(kSelThreads) void evict_select_kernel(float* __rest
       for (int j = 0; j < STEPS; ++j) keys[j] = weight_key(__uint_as_float(keys[j]));
     }
     // f(place, key) for this lane's places, in order; a place behind the last candidate has place >= cand
+    auto again = [&](auto f) __attribute__((always_inline)) {
+      constexpr int U = 8;
+#pragma unroll 1
+      for (int j0 = 0; j0 < steps; j0 += U) {
+        float x[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) x[u] = w[first + (j0 + u) * 64 < cand ? first + (j0 + u) * 64 : cand - 1];
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+          if (j0 + u < steps) f(first + (j0 + u) * 64, weight_key(x[u]));
+      }
+    };
     auto each = [&](auto f) __attribute__((always_inline)) {
       if constexpr (STEPS > 0) {
 #pragma unroll
         for (int j = 0; j < STEPS; ++j) f(first + j * 64, keys[j]);
       } else {
-        constexpr int U = 8;
-        for (int j0 = 0; j0 < steps; j0 += U) {
-          float x[U];
-#pragma unroll
-          for (int u = 0; u < U; ++u) x[u] = w[first + (j0 + u) * 64 < cand ? first + (j0 + u) * 64 : cand - 1];
-#pragma unroll
-          for (int u = 0; u < U; ++u)
-            if (j0 + u < steps) f(first + (j0 + u) * 64, weight_key(x[u]));
-        }
+        again(f);
       }
     };
     uint32_t prefix = 0, left = (uint32_t)keep;
@@ -107,6 +111,7 @@ __global__ __launch_bounds__(kSelThreads) void evict_select_kernel(float* __rest
         if (above < left && above + h[e] >= left) {
           s_prefix = prefix | (uint32_t)(kBins - 1 - 2 * tid - e) << shift;
           s_left = left - above;
+          s_equal = h[e];
         }
         above += h[e];
       }
@@ -116,46 +121,64 @@ __global__ __launch_bounds__(kSelThreads) void evict_select_kernel(float* __rest
     });
     // kept: above the key, or equal to it and among the first `left` of those
     const uint64_t below = (1ull << lane) - 1;
-    int equal = 0;
-    each([&](int i, uint32_t k) __attribute__((always_inline)) { equal += __popcll(__builtin_amdgcn_ballot_w64(i < cand && k == prefix)); });
-    if (lane == 0) s_wave[1][wave] = equal;
-    __syncthreads();
-    int before = 0;
-    for (int x = 0; x < kSelWaves; ++x) before += x < wave ? s_wave[1][x] : 0;
-    // f(place, whether it is given up among the first `keep` places, whether it is kept behind them, this lane's masks of both)
-    auto marks = [&](auto f) __attribute__((always_inline)) {
-      int rank0 = before;
-      each([&](int i, uint32_t k) __attribute__((always_inline)) {
-        const uint64_t eq = __builtin_amdgcn_ballot_w64(i < cand && k == prefix);
-        const bool kept = i < cand && (k > prefix || (k == prefix && rank0 + __popcll(eq & below) < (int)left));
-        rank0 += __popcll(eq);
-        const bool hole = i < keep && !kept, filler = i >= keep && kept;
-        f(i, hole, filler, __builtin_amdgcn_ballot_w64(hole), __builtin_amdgcn_ballot_w64(filler));
+    // Lists in order, from what each wave has of them.  walk(f): f(place, given up among the first `keep` places, kept behind them) for this lane's
+    // places in order.
+    auto lists = [&](auto walk) __attribute__((always_inline)) {
+      int holes = 0, fillers = 0;
+      walk([&](int, bool hole, bool filler) __attribute__((always_inline)) {
+        holes += hole;
+        fillers += filler;
+      });
+      for (int off = 32; off; off >>= 1) {
+        holes += __shfl_xor(holes, off, 64);
+        fillers += __shfl_xor(fillers, off, 64);
+      }
+      if (lane == 0) {
+        s_wave[0][wave] = holes;
+        s_wave[1][wave] = fillers;
+      }
+      __syncthreads();
+      holes = fillers = 0;
+      for (int x = 0; x < kSelWaves; ++x) {
+        holes += x < wave ? s_wave[0][x] : 0;
+        fillers += x < wave ? s_wave[1][x] : 0;
+        moves += s_wave[1][x];
+      }
+      walk([&](int i, bool hole, bool filler) __attribute__((always_inline)) {
+        const uint64_t h = __builtin_amdgcn_ballot_w64(hole), f = __builtin_amdgcn_ballot_w64(filler);
+        if (hole) to[holes + __popcll(h & below)] = i;
+        if (filler) from[fillers + __popcll(f & below)] = i;
+        holes += __popcll(h);
+        fillers += __popcll(f);
       });
     };
-    int holes = 0, fillers = 0;
-    marks([&](int, bool, bool, uint64_t h, uint64_t f) __attribute__((always_inline)) {
-      holes += __popcll(h);
-      fillers += __popcll(f);
-    });
-    __syncthreads();
-    if (lane == 0) {
-      s_wave[0][wave] = holes;
-      s_wave[1][wave] = fillers;
+    if (s_equal == left) {  // all of those that equal the key
+      lists([&](auto f) __attribute__((always_inline)) {
+        each([&](int i, uint32_t k) __attribute__((always_inline)) { f(i, i < keep && k < prefix, i >= keep && i < cand && k >= prefix); });
+      });
+    } else {  // some: by their ranks (masks of a lane's many places take more code than the row's second reading takes time)
+      auto stream = [&](auto f) __attribute__((always_inline)) {
+        if constexpr (STEPS > 10) again(f);
+        else each(f);
+      };
+      int equal = 0;
+      stream([&](int i, uint32_t k) __attribute__((always_inline)) { equal += i < cand && k == prefix; });
+      for (int off = 32; off; off >>= 1) equal += __shfl_xor(equal, off, 64);
+      if (lane == 0) s_wave[1][wave] = equal;
+      __syncthreads();
+      int before = 0;
+      for (int x = 0; x < kSelWaves; ++x) before += x < wave ? s_wave[1][x] : 0;
+      __syncthreads();
+      lists([&](auto f) __attribute__((always_inline)) {
+        int rank0 = before;
+        stream([&](int i, uint32_t k) __attribute__((always_inline)) {
+          const uint64_t eq = __builtin_amdgcn_ballot_w64(i < cand && k == prefix);
+          const bool kept = i < cand && (k > prefix || (k == prefix && rank0 + __popcll(eq & below) < (int)left));
+          rank0 += __popcll(eq);
+          f(i, i < keep && !kept, i >= keep && kept);
+        });
+      });
     }
-    __syncthreads();
-    holes = fillers = 0;
-    for (int x = 0; x < kSelWaves; ++x) {
-      holes += x < wave ? s_wave[0][x] : 0;
-      fillers += x < wave ? s_wave[1][x] : 0;
-      moves += s_wave[1][x];
-    }
-    marks([&](int i, bool hole, bool filler, uint64_t h, uint64_t f) __attribute__((always_inline)) {
-      if (hole) to[holes + __popcll(h & below)] = i;
-      if (filler) from[fillers + __popcll(f & below)] = i;
-      holes += __popcll(h);
-      fillers += __popcll(f);
-    });
     __syncthreads();
   }
   if (tid == 0) {
@@ -283,6 +306,10 @@ hipError_t launch_evict(void* k, void* v, float* weight, int32_t* positions, int
     evict_select_kernel<decltype(steps)::value><<<(unsigned)rows, kSelThreads, 0, stream>>>(weight, positions, lens, budgets, N, (int)budget, (int)recent,
                                                                                           (int32_t*)scratch, words);
   };
+#ifdef PKV_STREAM
+  if (1) select(std::integral_constant<int, 0>{});
+  else
+#endif
   if (most <= 2 * kSelThreads) select(std::integral_constant<int, 2>{});
   else if (most <= 5 * kSelThreads) select(std::integral_constant<int, 5>{});
   else if (most <= 10 * kSelThreads) select(std::integral_constant<int, 10>{});
