@@ -15,17 +15,18 @@ constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kNegInf = -__builtin_huge_valf();
 constexpr float kLow = -1.0e30f;        // a reference below every logit that counts
 constexpr int kTile = 32;               // keys per step of a wave
+constexpr float kMostSum = 4096.0f;     // of a lane's eight probabilities relative to its query's reference: within fp16, and nothing below is lost
 constexpr int kXcds = 8;
 constexpr int64_t kKeptQueries = 16;    // up to this many queries per key, logits are kept for the account
 
 template <bool F16>
 struct Elem {
-  static __device__ __forceinline__ float wide(uint32_t b) { return F16 ? (float)__builtin_bit_cast(_Float16, (uint16_t)b) : bf16_bits_to_f32((uint16_t)b); }
   static __device__ __forceinline__ uint16_t narrow(float f) {
     if constexpr (F16) return __builtin_bit_cast(uint16_t, (_Float16)f);
     else return f32_to_bf16_bits(f);
   }
   static constexpr uint32_t kExp = F16 ? 0x7c00u : 0x7f80u;  // all ones: not finite
+  static constexpr uint32_t kOne = F16 ? 0x3c00u : 0x3f80u;
   static __device__ __forceinline__ f32x4 mfma(u32x4 a, u32x4 b, f32x4 c) {
     if constexpr (F16) return mfma_f16_16x16x32(as_f16x8(a), as_f16x8(b), c);
     else return mfma_bf16_16x16x32(as_bf16x8(a), as_bf16x8(b), c);
@@ -107,12 +108,13 @@ __device__ __forceinline__ void read_transposed(uint32_t at, int d0, u32x4 (&f)[
 // A block's share: keys [begin, end) of a row for 16 * CT * W queries, of which each of the W waves has 16 * CT.  The waves share the keys' tiles.
 template <int D, bool F16, int CT, int W>
 struct Part {
+  static constexpr int SUB = W == 8 ? 2 : 1, KEYS = kTile * SUB;  // tiles, keys of a stage
   using E = Elem<F16>;
   static constexpr int CPR = D / 8, KK = D / 32, DT = D / 16;  // 16-byte pieces per key; products' steps; output tiles
-  static constexpr int NL = kTile * CPR / 64;                  // a tile's loads of K, by a wave
+  static constexpr int NL = KEYS * CPR / 64;                   // a stage's loads of K, by a wave
   static constexpr int STAGES = W == 1 ? 2 : 3, STAGE = 2 * NL * 64;
-  static constexpr int MINE = 2 * NL / W;                      // loads of a wave per tile
-  static_assert(MINE * W == 2 * NL, "the waves share a tile's loads");
+  static constexpr int MINE = 2 * NL / W;                      // loads of a wave per stage
+  static_assert(MINE * W == 2 * NL, "the waves share a stage's loads");
 
   static __device__ __forceinline__ void run(const AttendArgs& a, const Plan& p, const Keys& ks, bool shared, int64_t row, int split, int tile0, u32x4* lds) {
     const int lane = threadIdx.x & 63, wave = W == 1 ? 0 : __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), col = lane & 15, quad = lane >> 4;
@@ -136,7 +138,7 @@ struct Part {
       least = seen(len, T, w0 / T == w1 / T ? w0 % T : 0);
     }
     const int begin = split * ks.chunk, end = begin + ks.chunk < most ? begin + ks.chunk : most;
-    const int n_tiles = end > begin ? (end - begin + kTile - 1) / kTile : 0;
+    const int n_stages = end > begin ? (end - begin + KEYS - 1) / KEYS : 0;
 
     float m_run[CT], l_run[CT];
     f32x4 o[DT][CT];
@@ -147,7 +149,7 @@ struct Part {
 #pragma unroll
       for (int d = 0; d < DT; ++d) o[d][ct] = f32x4{0, 0, 0, 0};
     }
-    if (n_tiles > 0) {
+    if (n_stages > 0) {
       u32x4 bq[CT][KK];
 #pragma unroll
       for (int ct = 0; ct < CT; ++ct)
@@ -157,12 +159,12 @@ struct Part {
       const uint8_t* vb = (const uint8_t*)(shared ? a.v_shared : a.v) + ((size_t)row * ks.n + begin) * (D * 2);
       typedef const __attribute__((address_space(1))) void* gptr_t;
       typedef __attribute__((address_space(3))) void* lptr_t;
-      // Tile t straight into LDS, a key's pieces exchanged (swizzle) so that fragments are read from all banks.  Keys behind the last are the
+      // Stage t straight into LDS, a key's pieces exchanged (swizzle) so that fragments are read from all banks.  Keys behind the last are the
       // last one again: nothing behind it is touched.
       auto fetch = [&](int t, int stage) __attribute__((always_inline)) {
         u32x4* st = lds + stage * STAGE;
-        const int last = end - 1 - begin - t * kTile;
-        const uint8_t *kt = kb + (size_t)t * (kTile * D * 2), *vt = vb + (size_t)t * (kTile * D * 2);
+        const int last = end - 1 - begin - t * KEYS;
+        const uint8_t *kt = kb + (size_t)t * (KEYS * D * 2), *vt = vb + (size_t)t * (KEYS * D * 2);
 #pragma unroll
         for (int i = 0; i < MINE; ++i) {
           const int j = wave * MINE + i, jk = j < NL ? j : j - NL;  // piece j: NL of K, then NL of V
@@ -170,9 +172,8 @@ struct Part {
           __builtin_amdgcn_global_load_lds((gptr_t)((j < NL ? kt : vt) + at), (lptr_t)(st + j * 64), 16, 0, 0);
         }
       };
-      auto tile = [&](int t, const u32x4* st, auto cut_c) __attribute__((always_inline)) {
+      auto tile = [&](int n0, const u32x4* st, auto cut_c) __attribute__((always_inline)) {  // keys from n0 on
         constexpr bool cut = decltype(cut_c)::value;
-        const int n0 = begin + t * kTile;
         // S^T: a lane has the logits of its query (column) with keys 4 quad + r and 16 + 4 quad + r
         f32x4 s[2][CT];
 #pragma unroll
@@ -211,23 +212,30 @@ struct Part {
             x[i] = s[i >> 2][ct][i & 3];
             if constexpr (cut) x[i] = n0 + (i >> 2) * 16 + quad * 4 + (i & 3) < see[ct] ? x[i] : kNegInf;
           }
-          float top = max3f(x[0], x[1], x[2]);
-          top = max3f(top, x[3], x[4]);
-          top = max3f(top, x[5], x[6]);
-          top = quads_max(__builtin_fmaxf(top, x[7])) * c;
-          // the reference moves only where a logit lies 2^8 above it: probabilities up to that lose nothing
-          if (__builtin_amdgcn_ballot_w64(top > m_run[ct] + 8.0f)) {
+          // Probabilities by the reference that there is; only where some of a lane's come to more than kMostSum are the logits' maxima
+          // taken, the reference moved and the probabilities computed again (at first always).
+          auto probabilities = [&]() __attribute__((always_inline)) {
+            float sum = 0.0f;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+              pf[ct][i] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[i], c, -m_run[ct]));
+              sum += pf[ct][i];
+            }
+            return sum;
+          };
+          float sum = probabilities();
+          if (__builtin_amdgcn_ballot_w64(!(sum <= kMostSum))) {
+            asm volatile("");  // (without it the compiler scales the output in front of the branch)
+            float top = max3f(x[0], x[1], x[2]);
+            top = max3f(top, x[3], x[4]);
+            top = max3f(top, x[5], x[6]);
+            top = quads_max(__builtin_fmaxf(top, x[7])) * c;
             const float m = __builtin_fmaxf(m_run[ct], top), f = __builtin_amdgcn_exp2f(m_run[ct] - m);
             m_run[ct] = m;
             l_run[ct] *= f;
 #pragma unroll
             for (int d = 0; d < DT; ++d) o[d][ct] *= f;
-          }
-          float sum = 0.0f;
-#pragma unroll
-          for (int i = 0; i < 8; ++i) {
-            pf[ct][i] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[i], c, -m_run[ct]));
-            sum += pf[ct][i];
+            sum = probabilities();
           }
           l_run[ct] += sum;
 #pragma unroll
@@ -266,48 +274,74 @@ struct Part {
             for (int ct = 0; ct < CT; ++ct) o[d0 + i][ct] = E::mfma(v[i], lo[ct], o[d0 + i][ct]);
         }
         if constexpr (cut) {
-          if (__builtin_amdgcn_ballot_w64(bad)) {  // they meet those that do, one by one
+          if (__builtin_amdgcn_ballot_w64(bad)) {
+            // How many values of plus and of minus infinity (a NaN is both) each output would have met: products of ones, by queries that see the key.
+            uint32_t ones[CT][4];
 #pragma unroll
             for (int ct = 0; ct < CT; ++ct)
 #pragma unroll
-              for (int i = 0; i < 8; ++i)
-#pragma unroll 1
-                for (int qd = 0; qd < 4; ++qd) {
-                  const int j = (i >> 2) * 16 + qd * 4 + (i & 3);
-                  const float pj = __shfl(pf[ct][i], qd * 16 + col, 64);
-                  const bool sees = n0 + j < see[ct];
+              for (int i = 0; i < 4; ++i) {
+                const int n = n0 + (i >> 1) * 16 + quad * 4 + (i & 1) * 2;
+                ones[ct][i] = (n < see[ct] ? E::kOne : 0u) | (n + 1 < see[ct] ? E::kOne << 16 : 0u);
+              }
 #pragma unroll
-                  for (int d = 0; d < DT; ++d) {
-                    const int f = d * 16 + quad * 4;
-                    const u32x2 y = *reinterpret_cast<const u32x2*>((const uint16_t*)(vst + j * CPR + ((f >> 3) ^ swizzle<D>(j))) + (f & 7));
+            for (int d0 = 0; d0 < DT; d0 += 4) {
+              u32x4 v[4];
+              read_transposed<16 * D * 2>(at, d0, v);
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                      const uint32_t x = e & 1 ? y[e >> 1] >> 16 : y[e >> 1] & 0xffffu;
-                      if (sees && (x & E::kExp) == E::kExp) o[d][ct][e] = __builtin_fmaf(pj, E::wide(x), o[d][ct][e]);
-                    }
+              for (int i = 0; i < 4; ++i) {
+                u32x4 up, down;
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                  uint32_t u = 0, w = 0;
+#pragma unroll
+                  for (int sh = 0; sh < 32; sh += 16) {
+                    const uint32_t x = v[i][j] >> sh & 0xffffu;
+                    const bool odd = (x & E::kExp) == E::kExp;
+                    u |= odd && x != (E::kExp | 0x8000u) ? E::kOne << sh : 0u;
+                    w |= odd && x != E::kExp ? E::kOne << sh : 0u;
                   }
+                  up[j] = u;
+                  down[j] = w;
                 }
+#pragma unroll
+                for (int ct = 0; ct < CT; ++ct) {
+                  const u32x4 m = {ones[ct][0], ones[ct][1], ones[ct][2], ones[ct][3]};
+                  const f32x4 tu = E::mfma(up, m, f32x4{0, 0, 0, 0}), td = E::mfma(down, m, f32x4{0, 0, 0, 0});
+#pragma unroll
+                  for (int e = 0; e < 4; ++e) o[d0 + i][ct][e] += (tu[e] > 0.0f ? -kNegInf : 0.0f) + (td[e] > 0.0f ? kNegInf : 0.0f);
+                }
+              }
+            }
           }
         }
       };
-      fetch(0, 0);
-      if (n_tiles > 1) fetch(1, 1);
-      int stage = 0;
-      for (int t = 0; t < n_tiles; ++t) {
-        // this wave's part of tile t has landed; its loads of tile t + 1 may be under way
-        if (t + 1 < n_tiles) __builtin_amdgcn_s_waitcnt(MINE == 16 ? 0x4F70 : 0x0F70 | MINE);
-        else __builtin_amdgcn_s_waitcnt(0x0F70);
+      // waits until this wave's part of stage t has landed; its loads of stage t + 1 may be under way
+      auto landed = [&](int t) __attribute__((always_inline)) {
+        __builtin_amdgcn_s_waitcnt(MINE == 16 ? 0x4F70 : 0x0F70 | MINE);  // (on every path: it is where the compiler knows of the queries)
+        if (t + 1 >= n_stages) __builtin_amdgcn_s_waitcnt(0x0F70);
         asm volatile("" ::: "memory");
+      };
+      fetch(0, 0);
+      if (n_stages > 1) fetch(1, 1);
+      landed(0);  // and with it the queries: where the compiler does not know, it waits for all loads in front of every stage's products
+      int stage = 0;
+      for (int t = 0; t < n_stages; ++t) {
+        landed(t);
         if constexpr (W > 1) {
-          __builtin_amdgcn_s_barrier();  // everyone's has, and everyone has read tile t - 1, whose place takes tile t + 2
+          __builtin_amdgcn_s_barrier();  // everyone's has, and everyone has read stage t - 1, whose place takes stage t + 2
           asm volatile("" ::: "memory");
-          if (t + 2 < n_tiles) fetch(t + 2, stage == 0 ? 2 : stage - 1);
+          if (t + 2 < n_stages) fetch(t + 2, stage == 0 ? 2 : stage - 1);
         }
-        const u32x4* st = lds + stage * STAGE;
-        if (begin + (t + 1) * kTile <= least && begin + (t + 1) * kTile <= end) tile(t, st, std::integral_constant<bool, false>{});
-        else tile(t, st, std::integral_constant<bool, true>{});
-        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // all of tile t has been read
-        if (W == 1 && t + 2 < n_tiles) fetch(t + 2, stage);
+#pragma unroll 1
+        for (int sub = 0; sub < SUB; ++sub) {
+          const int n0 = begin + t * KEYS + sub * kTile;
+          const u32x4* st = lds + stage * STAGE + sub * (kTile * CPR);
+          if (n0 + kTile <= least && n0 + kTile <= end) tile(n0, st, std::integral_constant<bool, false>{});
+          else if (n0 < end) tile(n0, st, std::integral_constant<bool, true>{});
+        }
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // all of stage t has been read
+        if (W == 1 && t + 2 < n_stages) fetch(t + 2, stage);
         stage = stage == STAGES - 1 ? 0 : stage + 1;
       }
     }
@@ -317,7 +351,7 @@ struct Part {
       const float l = quads_sum(l_run[ct]);
       if (m0 + ct * 16 + col < M) {
         if (quad == 0) reinterpret_cast<float2*>(p.ml)[at + query[ct]] = float2{m_run[ct], l};
-        if (n_tiles > 0) {
+        if (n_stages > 0) {
 #pragma unroll
           for (int d = 0; d < DT; ++d) *reinterpret_cast<f32x4*>(p.o + (at + query[ct]) * D + d * 16 + quad * 4) = o[d][ct];
         }
@@ -488,18 +522,20 @@ __global__ __launch_bounds__(256) void attend_finish_kernel(AttendArgs a, Plan p
   }
 }
 
-// The account where the logits were not kept: a wave holds 64 keys and walks the queries that see them, 16 at a time.  S: a lane has the
-// logits of its key (column) with queries 4 quad + r.
+// The account where the logits were not kept: a block takes 128 keys of a row and walks the queries that see them, 64 at a time, which all
+// its waves have in LDS: two waves take 64 keys each with one half of those, two with the other.  S: a lane has the logits of its
+// key (column) with queries 4 quad + r, so that a key's sum stays in the lane until the end.
 template <int D, bool F16>
-__global__ __launch_bounds__(256) void attend_account_kernel(AttendArgs a, Keys ks, bool shared, const float* __restrict__ lse) {
+__global__ __launch_bounds__(256, 2) void attend_account_kernel(AttendArgs a, Keys ks, bool shared, const float* __restrict__ lse) {
   using E = Elem<F16>;
-  constexpr int KK = D / 32;
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, col = lane & 15, quad = lane >> 4;
-  const int per = (int)(a.group * a.T), T = (int)a.T, M = (int)ks.m, blocks = (int)((ks.n + 255) / 256);
+  constexpr int CPR = D / 8, KK = D / 32, QS = 64, STAGE = QS * CPR + QS / 4, LOADS = QS * CPR / 256;  // queries, 16-byte units and a wave's loads of a step
+  __shared__ u32x4 lds[3 * STAGE];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), col = lane & 15, quad = lane >> 4;
+  const int per = (int)(a.group * a.T), T = (int)a.T, M = (int)ks.m, blocks = (int)((ks.n + 127) / 128);
   const int64_t row = blockIdx.x / blocks;
-  const int n0 = blockIdx.x % blocks * 256 + wave * 64;
+  const int b0 = blockIdx.x % blocks * 128, n0 = b0 + (wave & 1) * 64, half = wave >> 1;
   const int len = row_len(shared ? a.shared_lens : a.lens, row, ks.n);
-  if (n0 >= len) return;
+  if (b0 >= len) return;
   const float c = kLog2e / __builtin_sqrtf((float)D);
   u32x4 bk[4][KK];
 #pragma unroll
@@ -509,36 +545,94 @@ __global__ __launch_bounds__(256) void attend_account_kernel(AttendArgs a, Keys 
 #pragma unroll
     for (int kk = 0; kk < KK; ++kk) bk[kt][kk] = *reinterpret_cast<const u32x4*>(k + kk * 32);
   }
-  float sum[4] = {};
-  for (int q0 = 0; q0 < M; q0 += 16) {
-    const int mq = q0 + col < M ? q0 + col : M - 1;
-    const uint16_t* q = (const uint16_t*)a.q + query_at(shared, row, mq, per, a.heads) * D + quad * 8;
-    u32x4 fq[KK];
+  typedef const __attribute__((address_space(1))) void* gptr_t;
+  typedef __attribute__((address_space(3))) void* lptr_t;
+  const int steps = (M + QS - 1) / QS;
+  auto fetch = [&](int t, int stage) __attribute__((always_inline)) {
+    u32x4* st = lds + stage * STAGE;
 #pragma unroll
-    for (int kk = 0; kk < KK; ++kk) fq[kk] = *reinterpret_cast<const u32x4*>(q + kk * 32);
-    float ref[4];
-    int see[4];
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      const int m = q0 + quad * 4 + e;
-      ref[e] = m < M ? lse[row * M + m] : -kNegInf;
-      see[e] = shared ? len : seen(len, T, m % T);
+    for (int i = 0; i < LOADS; ++i) {
+      const int j = wave * LOADS + i, r = j * (64 / CPR) + lane / CPR, m = t * QS + r < M ? t * QS + r : M - 1;
+      const uint16_t* q = (const uint16_t*)a.q + query_at(shared, row, m, per, a.heads) * D + ((lane % CPR) ^ swizzle<D>(r)) * 8;
+      __builtin_amdgcn_global_load_lds((gptr_t)q, (lptr_t)(st + j * 64), 16, 0, 0);
     }
+    // every wave, so that all have as many loads under way
+    const int m = t * QS + lane < M ? t * QS + lane : M - 1;
+    __builtin_amdgcn_global_load_lds((gptr_t)(lse + row * M + m), (lptr_t)(st + QS * CPR), 4, 0, 0);
+  };
+  float sum[4] = {};
+  auto step = [&](int q0, const u32x4* st, auto cut_c) __attribute__((always_inline)) {
+    constexpr bool cut = decltype(cut_c)::value;
+#pragma unroll
+    for (int rt = 0; rt < QS / 32; ++rt) {
+      const int r0 = half * (QS / 2) + rt * 16, r = r0 + col;
+      u32x4 fq[KK];
+#pragma unroll
+      for (int kk = 0; kk < KK; ++kk) fq[kk] = st[r * CPR + ((kk * 4 + quad) ^ swizzle<D>(r))];
+      const f32x4 ref = reinterpret_cast<const f32x4*>(st + QS * CPR)[r0 / 4 + quad];
+      f32x4 s[4];
+#pragma unroll
+      for (int kt = 0; kt < 4; ++kt) s[kt] = f32x4{0, 0, 0, 0};
+#pragma unroll
+      for (int kk = 0; kk < KK; ++kk)
+#pragma unroll
+        for (int kt = 0; kt < 4; ++kt) s[kt] = E::mfma(fq[kk], bk[kt][kk], s[kt]);
+      int see[4];
+      if constexpr (cut) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const int m = q0 + r0 + quad * 4 + e;
+          see[e] = m >= M ? 0 : shared ? len : seen(len, T, m % T);
+        }
+      }
+#pragma unroll
+      for (int kt = 0; kt < 4; ++kt)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const float x = __builtin_amdgcn_exp2f(__builtin_fmaf(s[kt][e], c, -ref[e]));
+          sum[kt] += !cut || n0 + kt * 16 + col < see[e] ? x : 0.0f;
+        }
+    }
+  };
+  // waits until this wave's part of step t has landed
+  auto landed = [&](int t) __attribute__((always_inline)) {
+    __builtin_amdgcn_s_waitcnt(0x0F70 | (LOADS + 1));  // (on every path: it is where the compiler knows of the keys)
+    if (t + 1 >= steps) __builtin_amdgcn_s_waitcnt(0x0F70);
+    asm volatile("" ::: "memory");
+  };
+  fetch(0, 0);
+  if (steps > 1) fetch(1, 1);
+  landed(0);  // and with it the resident keys: where the compiler does not know, it waits for all loads in front of every step's products
+  int stage = 0;
+  for (int t = 0; t < steps; ++t) {
+    landed(t);
+    __builtin_amdgcn_s_barrier();  // everyone's has, and everyone has read step t - 1, whose place takes step t + 2
+    asm volatile("" ::: "memory");
+    if (t + 2 < steps) fetch(t + 2, stage == 0 ? 2 : stage - 1);
+    // whether all the step's queries see all of this wave's keys
+    const int q0 = t * QS, q1 = q0 + QS - 1;
+    const int least = shared ? len : seen(len, T, q0 / T == q1 / T ? q0 % T : 0);
+    if (q1 < M && n0 + 64 <= least) step(q0, lds + stage * STAGE, std::integral_constant<bool, false>{});
+    else step(q0, lds + stage * STAGE, std::integral_constant<bool, true>{});
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    stage = stage == 2 ? 0 : stage + 1;
+  }
+  __syncthreads();
+  float* w = (shared ? a.weight_shared : a.weight) + row * ks.n;
+  float* other = reinterpret_cast<float*>(lds);
+#pragma unroll
+  for (int kt = 0; kt < 4; ++kt) sum[kt] = quads_sum(sum[kt]);
+  if (half == 1 && quad == 0) {
+#pragma unroll
+    for (int kt = 0; kt < 4; ++kt) other[(wave & 1) * 64 + kt * 16 + col] = sum[kt];
+  }
+  __syncthreads();
+  if (half == 0 && quad == 0) {
 #pragma unroll
     for (int kt = 0; kt < 4; ++kt) {
-      f32x4 s = {0, 0, 0, 0};
-#pragma unroll
-      for (int kk = 0; kk < KK; ++kk) s = E::mfma(fq[kk], bk[kt][kk], s);
-#pragma unroll
-      for (int e = 0; e < 4; ++e) sum[kt] += n0 + kt * 16 + col < see[e] ? __builtin_amdgcn_exp2f(__builtin_fmaf(s[e], c, -ref[e])) : 0.0f;
+      const int n = n0 + kt * 16 + col;
+      if (n < len) w[n] += sum[kt] + other[(wave & 1) * 64 + kt * 16 + col];
     }
-  }
-  float* w = (shared ? a.weight_shared : a.weight) + row * ks.n;
-#pragma unroll
-  for (int kt = 0; kt < 4; ++kt) {
-    const float x = quads_sum(sum[kt]);
-    const int n = n0 + kt * 16 + col;
-    if (quad == 0 && n < len) w[n] += x;
   }
 }
 
@@ -640,11 +734,11 @@ hipError_t launch_attend_of(const AttendArgs& a, void* scratch, hipStream_t stre
   else finish_of(std::integral_constant<int, 1>{});
   e = hipGetLastError();
   if (e == hipSuccess && a.weight_shared != nullptr && !p.shared.scores) {
-    attend_account_kernel<D, F16><<<(unsigned)(p.shared.rows * ((p.shared.n + 255) / 256)), 256, 0, stream>>>(a, p.shared, true, p.lse + p.queries);
+    attend_account_kernel<D, F16><<<(unsigned)(p.shared.rows * ((p.shared.n + 127) / 128)), 256, 0, stream>>>(a, p.shared, true, p.lse + p.queries);
     e = hipGetLastError();
   }
   if (e == hipSuccess && a.weight != nullptr && p.own.n > 0 && !p.own.scores) {
-    attend_account_kernel<D, F16><<<(unsigned)(p.own.rows * ((p.own.n + 255) / 256)), 256, 0, stream>>>(a, p.own, false, p.lse);
+    attend_account_kernel<D, F16><<<(unsigned)(p.own.rows * ((p.own.n + 127) / 128)), 256, 0, stream>>>(a, p.own, false, p.lse);
     e = hipGetLastError();
   }
   return e;
