@@ -108,11 +108,11 @@ __device__ __forceinline__ void read_transposed(uint32_t at, int d0, u32x4 (&f)[
 // A block's share: keys [begin, end) of a row for 16 * CT * W queries, of which each of the W waves has 16 * CT.  The waves share the keys' tiles.
 template <int D, bool F16, int CT, int W>
 struct Part {
-  static constexpr int SUB = W == 8 ? 2 : 1, KEYS = kTile * SUB;  // tiles, keys of a stage
+  static constexpr int SUB = W > 1 ? 2 : 1, KEYS = kTile * SUB;  // tiles, keys of a stage
   using E = Elem<F16>;
   static constexpr int CPR = D / 8, KK = D / 32, DT = D / 16;  // 16-byte pieces per key; products' steps; output tiles
   static constexpr int NL = KEYS * CPR / 64;                   // a stage's loads of K, by a wave
-  static constexpr int STAGES = W == 1 ? 2 : 3, STAGE = 2 * NL * 64;
+  static constexpr int STAGES = 2, STAGE = 2 * NL * 64;
   static constexpr int MINE = 2 * NL / W;                      // loads of a wave per stage
   static_assert(MINE * W == 2 * NL, "the waves share a stage's loads");
 
@@ -122,7 +122,7 @@ struct Part {
     const int b0 = tile0 * 16 * CT * W, m0 = b0 + wave * 16 * CT;
     const float c = kLog2e / __builtin_sqrtf((float)D);
     const int len = row_len(shared ? a.shared_lens : a.lens, row, ks.n);
-    // keys that all, and that any, of the block's (most) and of the wave's queries (least) see
+    // keys that all, and that any, of the block's queries see
     int64_t query[CT];
     int see[CT];
     int least = len, most = len;
@@ -133,9 +133,10 @@ struct Part {
       see[ct] = shared ? len : seen(len, T, mc % T);
     }
     if (!shared) {
-      const int b1 = (b0 + 16 * CT * W < M ? b0 + 16 * CT * W : M) - 1, w0 = m0 < M ? m0 : M - 1, w1 = (m0 + 16 * CT < M ? m0 + 16 * CT : M) - 1;
-      most = seen(len, T, b0 / T == b1 / T ? b1 % T : T - 1);  // (tokens of one head, in order)
-      least = seen(len, T, w0 / T == w1 / T ? w0 % T : 0);
+      const int b1 = (b0 + 16 * CT * W < M ? b0 + 16 * CT * W : M) - 1;
+      const bool one = b0 / T == b1 / T;  // tokens of one head, in order
+      most = seen(len, T, one ? b1 % T : T - 1);
+      least = seen(len, T, one ? b0 % T : 0);
     }
     const int begin = split * ks.chunk, end = begin + ks.chunk < most ? begin + ks.chunk : most;
     const int n_stages = end > begin ? (end - begin + KEYS - 1) / KEYS : 0;
@@ -161,16 +162,17 @@ struct Part {
       typedef __attribute__((address_space(3))) void* lptr_t;
       // Stage t straight into LDS, a key's pieces exchanged (swizzle) so that fragments are read from all banks.  Keys behind the last are the
       // last one again: nothing behind it is touched.
+      const int r0 = wave * (64 / CPR) + lane / CPR, piece = (lane % CPR) ^ swizzle<D>(r0);
       auto fetch = [&](int t, int stage) __attribute__((always_inline)) {
-        u32x4* st = lds + stage * STAGE;
+        u32x4* st = lds + stage * STAGE + wave * 64;
         const int last = end - 1 - begin - t * KEYS;
         const uint8_t *kt = kb + (size_t)t * (KEYS * D * 2), *vt = vb + (size_t)t * (KEYS * D * 2);
-#pragma unroll
-        for (int i = 0; i < MINE; ++i) {
-          const int j = wave * MINE + i, jk = j < NL ? j : j - NL;  // piece j: NL of K, then NL of V
-          const int r = jk * (64 / CPR) + lane / CPR, at = (r < last ? r : last) * (D * 2) + ((lane % CPR) ^ swizzle<D>(r)) * 16;
-          __builtin_amdgcn_global_load_lds((gptr_t)((j < NL ? kt : vt) + at), (lptr_t)(st + j * 64), 16, 0, 0);
-        }
+        static_for<NL / W>([&](auto ic) __attribute__((always_inline)) {
+          constexpr int i = decltype(ic)::value, step = i * W * (64 / CPR), turn = D == 128 ? step & 15 : (step >> 1) & 7;  // (its bits are not r0's)
+          const int r = r0 + step, at = (r < last ? r : last) * (D * 2) + (piece ^ turn) * 16;
+          __builtin_amdgcn_global_load_lds((gptr_t)(kt + at), (lptr_t)(st + i * W * 64), 16, 0, 0);
+          __builtin_amdgcn_global_load_lds((gptr_t)(vt + at), (lptr_t)(st + (NL + i * W) * 64), 16, 0, 0);
+        });
       };
       auto tile = [&](int n0, const u32x4* st, auto cut_c) __attribute__((always_inline)) {  // keys from n0 on
         constexpr bool cut = decltype(cut_c)::value;
@@ -224,8 +226,7 @@ struct Part {
             return sum;
           };
           float sum = probabilities();
-          if (__builtin_amdgcn_ballot_w64(!(sum <= kMostSum))) {
-            asm volatile("");  // (without it the compiler scales the output in front of the branch)
+          if (__builtin_expect(__builtin_amdgcn_ballot_w64(!(sum <= kMostSum)) != 0, 0)) {
             float top = max3f(x[0], x[1], x[2]);
             top = max3f(top, x[3], x[4]);
             top = max3f(top, x[5], x[6]);
@@ -274,7 +275,7 @@ struct Part {
             for (int ct = 0; ct < CT; ++ct) o[d0 + i][ct] = E::mfma(v[i], lo[ct], o[d0 + i][ct]);
         }
         if constexpr (cut) {
-          if (__builtin_amdgcn_ballot_w64(bad)) {
+          if (__builtin_expect(__builtin_amdgcn_ballot_w64(bad) != 0, 0)) {
             // How many values of plus and of minus infinity (a NaN is both) each output would have met: products of ones, by queries that see the key.
             uint32_t ones[CT][4];
 #pragma unroll
@@ -316,34 +317,40 @@ struct Part {
           }
         }
       };
-      // waits until this wave's part of stage t has landed; its loads of stage t + 1 may be under way
-      auto landed = [&](int t) __attribute__((always_inline)) {
-        __builtin_amdgcn_s_waitcnt(MINE == 16 ? 0x4F70 : 0x0F70 | MINE);  // (on every path: it is where the compiler knows of the queries)
-        if (t + 1 >= n_stages) __builtin_amdgcn_s_waitcnt(0x0F70);
-        asm volatile("" ::: "memory");
-      };
+      // A wave alone has two stages under way; waves that share them ask for the next one when all of them have read the one before.
+      // (The waits are on every path: it is where the compiler knows that the queries have landed, for which it otherwise waits in every
+      // stage, and for the stages under way with them.)
       fetch(0, 0);
-      if (n_stages > 1) fetch(1, 1);
-      landed(0);  // and with it the queries: where the compiler does not know, it waits for all loads in front of every stage's products
-      int stage = 0;
-      for (int t = 0; t < n_stages; ++t) {
-        landed(t);
-        if constexpr (W > 1) {
-          __builtin_amdgcn_s_barrier();  // everyone's has, and everyone has read stage t - 1, whose place takes stage t + 2
-          asm volatile("" ::: "memory");
-          if (t + 2 < n_stages) fetch(t + 2, stage == 0 ? 2 : stage - 1);
-        }
+      if (W == 1 && n_stages > 1) fetch(1, 1);
+      __builtin_amdgcn_s_waitcnt(W == 1 ? MINE == 16 ? 0x4F70 : 0x0F70 | MINE : 0x0F70);
+      auto stages = [&](int t0, int t1, auto cut) __attribute__((always_inline)) {
+        for (int t = t0; t < t1; ++t) {
+          const int stage = t & 1;
+          if constexpr (W == 1) {  // stage t has landed; the loads of stage t + 1 may be under way
+            __builtin_amdgcn_s_waitcnt(MINE == 16 ? 0x4F70 : 0x0F70 | MINE);
+            if (t + 1 == n_stages) __builtin_amdgcn_s_waitcnt(0x0F70);
+            asm volatile("" ::: "memory");
+          } else {
+            __builtin_amdgcn_s_waitcnt(0x0F70);
+            asm volatile("" ::: "memory");
+            __builtin_amdgcn_s_barrier();  // everyone's part has, and everyone has read stage t - 1, whose place takes stage t + 1
+            asm volatile("" ::: "memory");
+            if (t + 1 < n_stages) fetch(t + 1, stage ^ 1);
+          }
 #pragma unroll 1
-        for (int sub = 0; sub < SUB; ++sub) {
-          const int n0 = begin + t * KEYS + sub * kTile;
-          const u32x4* st = lds + stage * STAGE + sub * (kTile * CPR);
-          if (n0 + kTile <= least && n0 + kTile <= end) tile(n0, st, std::integral_constant<bool, false>{});
-          else if (n0 < end) tile(n0, st, std::integral_constant<bool, true>{});
+          for (int sub = 0; sub < SUB; ++sub) {
+            const int n0 = begin + t * KEYS + sub * kTile;
+            if (!decltype(cut)::value || n0 < end) tile(n0, lds + stage * STAGE + sub * (kTile * CPR), cut);
+          }
+          asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // all of stage t has been read
+          if (W == 1 && t + 2 < n_stages) fetch(t + 2, stage);
         }
-        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // all of stage t has been read
-        if (W == 1 && t + 2 < n_stages) fetch(t + 2, stage);
-        stage = stage == STAGES - 1 ? 0 : stage + 1;
-      }
+      };
+      // whole stages that all of the block's queries see, and those behind them (a loop each: where one loop has both kinds of tiles, the
+      // compiler moves the outputs from register to register in every tile)
+      const int whole = least < end ? least : end, full = whole > begin ? (whole - begin) / KEYS : 0;
+      stages(0, full, std::integral_constant<bool, false>{});
+      stages(full, n_stages, std::integral_constant<bool, true>{});
     }
     const size_t at = (size_t)(ks.first_split + split) * p.queries;
 #pragma unroll
@@ -372,7 +379,7 @@ __device__ __forceinline__ bool share_of(int b, const Keys& ks, int64_t& row, in
 
 // Few queries per row: a wave each.  CT: of the kind of keys that has the larger tiles.
 template <int D, bool F16, int CT>
-__global__ __launch_bounds__(64, 1) void attend_wave_kernel(AttendArgs a, Plan p) {
+__global__ __launch_bounds__(64, CT == 1 ? 2 : 1) void attend_wave_kernel(AttendArgs a, Plan p) {
   __shared__ u32x4 lds[Part<D, F16, CT, 1>::STAGES * Part<D, F16, CT, 1>::STAGE];
   const bool shared = (int)blockIdx.x < p.shared.blocks;
   const Keys& ks = shared ? p.shared : p.own;
@@ -385,7 +392,7 @@ __global__ __launch_bounds__(64, 1) void attend_wave_kernel(AttendArgs a, Plan p
 
 // Many: W waves of 32 queries share the keys.
 template <int D, bool F16, int W>
-__global__ __launch_bounds__(64 * W, W < 4 ? 1 : W / 4) void attend_block_kernel(AttendArgs a, Plan p, bool shared) {
+__global__ __launch_bounds__(64 * W, W == 2 ? 1 : 2) void attend_block_kernel(AttendArgs a, Plan p, bool shared) {
   __shared__ u32x4 lds[Part<D, F16, 2, W>::STAGES * Part<D, F16, 2, W>::STAGE];
   const Keys& ks = shared ? p.shared : p.own;
   int64_t row;
@@ -524,7 +531,8 @@ __global__ __launch_bounds__(256) void attend_finish_kernel(AttendArgs a, Plan p
 
 // The account where the logits were not kept: a block takes 128 keys of a row and walks the queries that see them, 64 at a time, which all
 // its waves have in LDS: two waves take 64 keys each with one half of those, two with the other.  S: a lane has the logits of its
-// key (column) with queries 4 quad + r, so that a key's sum stays in the lane until the end.
+// key (column) with queries 4 quad + r, so that a key's sum stays in the lane until the end.  The products of the next 16 queries are
+// spread between the exponentials of the 16 before: one after the other, matrix and vector instructions of a SIMD's waves take turns.
 template <int D, bool F16>
 __global__ __launch_bounds__(256, 2) void attend_account_kernel(AttendArgs a, Keys ks, bool shared, const float* __restrict__ lse) {
   using E = Elem<F16>;
@@ -560,38 +568,39 @@ __global__ __launch_bounds__(256, 2) void attend_account_kernel(AttendArgs a, Ke
     const int m = t * QS + lane < M ? t * QS + lane : M - 1;
     __builtin_amdgcn_global_load_lds((gptr_t)(lse + row * M + m), (lptr_t)(st + QS * CPR), 4, 0, 0);
   };
+  struct Logits {
+    f32x4 s[4], ref;
+  };
   float sum[4] = {};
-  auto step = [&](int q0, const u32x4* st, auto cut_c) __attribute__((always_inline)) {
-    constexpr bool cut = decltype(cut_c)::value;
+  auto read = [&](u32x4 (&fq)[KK], Logits& x, const u32x4* st, int rt) __attribute__((always_inline)) {
+    const int r0 = half * (QS / 2) + rt * 16, r = r0 + col;
 #pragma unroll
-    for (int rt = 0; rt < QS / 32; ++rt) {
-      const int r0 = half * (QS / 2) + rt * 16, r = r0 + col;
-      u32x4 fq[KK];
+    for (int kk = 0; kk < KK; ++kk) fq[kk] = st[r * CPR + ((kk * 4 + quad) ^ swizzle<D>(r))];
+    x.ref = reinterpret_cast<const f32x4*>(st + QS * CPR)[r0 / 4 + quad];
+  };
+  auto products = [&](const u32x4 (&fq)[KK], Logits& x) __attribute__((always_inline)) {
 #pragma unroll
-      for (int kk = 0; kk < KK; ++kk) fq[kk] = st[r * CPR + ((kk * 4 + quad) ^ swizzle<D>(r))];
-      const f32x4 ref = reinterpret_cast<const f32x4*>(st + QS * CPR)[r0 / 4 + quad];
-      f32x4 s[4];
+    for (int kt = 0; kt < 4; ++kt) x.s[kt] = f32x4{0, 0, 0, 0};
 #pragma unroll
-      for (int kt = 0; kt < 4; ++kt) s[kt] = f32x4{0, 0, 0, 0};
+    for (int kk = 0; kk < KK; ++kk)
 #pragma unroll
-      for (int kk = 0; kk < KK; ++kk)
+      for (int kt = 0; kt < 4; ++kt) x.s[kt] = E::mfma(fq[kk], bk[kt][kk], x.s[kt]);
+  };
+  auto add = [&](const Logits& x) __attribute__((always_inline)) {
 #pragma unroll
-        for (int kt = 0; kt < 4; ++kt) s[kt] = E::mfma(fq[kk], bk[kt][kk], s[kt]);
-      int see[4];
-      if constexpr (cut) {
+    for (int kt = 0; kt < 4; ++kt)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const int m = q0 + r0 + quad * 4 + e;
-          see[e] = m >= M ? 0 : shared ? len : seen(len, T, m % T);
-        }
+      for (int e = 0; e < 4; ++e) sum[kt] += __builtin_amdgcn_exp2f(__builtin_fmaf(x.s[kt][e], c, -x.ref[e]));
+  };
+  auto add_cut = [&](const Logits& x, int q0, int rt) __attribute__((always_inline)) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const int m = q0 + half * (QS / 2) + rt * 16 + quad * 4 + e, see = m >= M ? 0 : shared ? len : seen(len, T, m % T);
+#pragma unroll
+      for (int kt = 0; kt < 4; ++kt) {
+        const float y = __builtin_amdgcn_exp2f(__builtin_fmaf(x.s[kt][e], c, -x.ref[e]));
+        sum[kt] += n0 + kt * 16 + col < see ? y : 0.0f;
       }
-#pragma unroll
-      for (int kt = 0; kt < 4; ++kt)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const float x = __builtin_amdgcn_exp2f(__builtin_fmaf(s[kt][e], c, -ref[e]));
-          sum[kt] += !cut || n0 + kt * 16 + col < see[e] ? x : 0.0f;
-        }
     }
   };
   // waits until this wave's part of step t has landed
@@ -603,20 +612,50 @@ __global__ __launch_bounds__(256, 2) void attend_account_kernel(AttendArgs a, Ke
   fetch(0, 0);
   if (steps > 1) fetch(1, 1);
   landed(0);  // and with it the resident keys: where the compiler does not know, it waits for all loads in front of every step's products
+  // Logits that wait for their exponentials go from one step to the next: none at first, which a reference of +infinity makes zeros of.
+  Logits pending;
+#pragma unroll
+  for (int kt = 0; kt < 4; ++kt) pending.s[kt] = f32x4{0, 0, 0, 0};
+  pending.ref = f32x4{-kNegInf, -kNegInf, -kNegInf, -kNegInf};
   int stage = 0;
   for (int t = 0; t < steps; ++t) {
     landed(t);
     __builtin_amdgcn_s_barrier();  // everyone's has, and everyone has read step t - 1, whose place takes step t + 2
     asm volatile("" ::: "memory");
     if (t + 2 < steps) fetch(t + 2, stage == 0 ? 2 : stage - 1);
+    const u32x4* st = lds + stage * STAGE;
     // whether all the step's queries see all of this wave's keys
     const int q0 = t * QS, q1 = q0 + QS - 1;
     const int least = shared ? len : seen(len, T, q0 / T == q1 / T ? q0 % T : 0);
-    if (q1 < M && n0 + 64 <= least) step(q0, lds + stage * STAGE, std::integral_constant<bool, false>{});
-    else step(q0, lds + stage * STAGE, std::integral_constant<bool, true>{});
+    if (q1 < M && n0 + 64 <= least) {
+      static_for<QS / 32>([&](auto rt) __attribute__((always_inline)) {
+        u32x4 fq[KK];
+        Logits next;
+        read(fq, next, st, decltype(rt)::value);
+        __builtin_amdgcn_sched_barrier(0);
+        products(fq, next);
+        add(pending);
+#pragma unroll
+        for (int i = 0; i < 4 * KK; ++i) {
+          __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);             // one product
+          __builtin_amdgcn_sched_group_barrier(0x002, 48 / (4 * KK), 0);  // its share of 16 fma, 16 exponentials and 16 additions
+        }
+        __builtin_amdgcn_sched_barrier(0);
+        pending = next;
+      });
+    } else {
+      static_for<QS / 32>([&](auto rt) __attribute__((always_inline)) {
+        u32x4 fq[KK];
+        Logits next;
+        read(fq, next, st, decltype(rt)::value);
+        products(fq, next);
+        add_cut(next, q0, decltype(rt)::value);
+      });
+    }
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
     stage = stage == 2 ? 0 : stage + 1;
   }
+  add(pending);
   __syncthreads();
   float* w = (shared ? a.weight_shared : a.weight) + row * ks.n;
   float* other = reinterpret_cast<float*>(lds);
