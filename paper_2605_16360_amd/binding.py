@@ -394,7 +394,7 @@ def proxykv_attend(ctx: Context, q, k, v, lens=None, weight=None, out=None, stre
     rows, (group, T, D), N = shape[:-3], shape[-3:], k.shape[-2]
     cache = rows + (N, D)
     if out is None:
-        out = torch.empty(shape, dtype=dt, device=q.device)
+        out = torch.empty_like(q)
     _check(load().proxykv_attend(ctx.handle, _arg("q", q, device, dt, shape), _arg("k", k, device, dt, cache), _arg("v", v, device, dt, cache),
                                  _arg("lens", lens, device, torch.int32, rows), _cache_dtype(q), rows.numel(), N, group, T, D,
                                  _arg("out", out, device, dt, shape), _arg("weight", weight, device, torch.float32, rows + (N,)),
@@ -416,7 +416,7 @@ def proxykv_attend_shared(ctx: Context, q, k_shared, v_shared, k=None, v=None, s
     P, N = k_shared.shape[-2], 0 if k is None else k.shape[-2]
     both, own = (heads, P, D), (batch, heads, N, D)
     if out is None:
-        out = torch.empty(shape, dtype=dt, device=q.device)
+        out = torch.empty_like(q)
     args = [_arg("q", q, device, dt, shape), _arg("k_shared", k_shared, device, dt, both), _arg("v_shared", v_shared, device, dt, both),
             _arg("shared_lens", shared_lens, device, torch.int32, (heads,)), _arg("k", k, device, dt, own), _arg("v", v, device, dt, own),
             _arg("lens", lens, device, torch.int32, (batch, heads))]

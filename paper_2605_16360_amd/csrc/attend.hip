@@ -7,6 +7,9 @@
 // computed once more.  No sum's order depends on timing.
 #include "common.hpp"
 #include "kernels.hpp"
+#ifndef PKV_BIG
+#define PKV_BIG 384
+#endif
 
 namespace pkv {
 namespace {
@@ -17,7 +20,7 @@ constexpr float kLow = -1.0e30f;        // a reference below every logit that co
 constexpr int kTile = 32;               // keys per step of a wave
 constexpr float kMostSum = 4096.0f;     // of a lane's eight probabilities relative to its query's reference: within fp16, and nothing below is lost
 constexpr int kXcds = 8;
-constexpr int64_t kKeptQueries = 16;    // up to this many queries per key, logits are kept for the account
+constexpr int64_t kKeptQueries = 32;    // up to this many queries per key, logits are kept for the account
 
 template <bool F16>
 struct Elem {
@@ -61,11 +64,18 @@ __device__ __forceinline__ int seen(int len, int T, int t) {
   return n < 0 ? 0 : n;
 }
 
+// m % T for 0 <= m < 2^23, which a float holds: inv = 1 / T is off by 2^-24 relative, so the quotient by one at most
+__device__ __forceinline__ int remainder_of(int m, int T, float inv) {
+  int r = m - (int)((float)m * inv) * T;
+  r += r < 0 ? T : 0;
+  return r >= T ? r - T : r;
+}
+
 // One kind of keys (shared or own) in a launch: `rows` rows of `n` keys, each seen by m queries, in `tiles` tiles of 16 * ct * waves, and cut into
-// `splits` shares of `chunk` keys.
+// `splits` shares of `chunk` keys, which `merge` waves cut once more.
 struct Keys {
   int64_t rows, n, m, score_stride;
-  int splits, chunk, tiles, ct, waves, blocks, first_split;
+  int splits, chunk, tiles, ct, waves, merge, blocks, first_split, parts;
   float* scores;  // [rows, m, score_stride] logits, or null
 };
 struct Plan {
@@ -75,6 +85,7 @@ struct Plan {
   float* ml;       // [splits, queries] pairs
   float* o;        // [splits, queries, D]
   float* lse;      // [queries] in the order of q, and behind them in the shared keys' order
+  float* part_sums;  // accounts of parts of the queries
 };
 
 // Where query m of a row's m queries lies in q.  Shared keys: row = head, queries (sequence, group head, token).
@@ -105,9 +116,11 @@ __device__ __forceinline__ void read_transposed(uint32_t at, int d0, u32x4 (&f)[
   for (int i = 0; i < 4; ++i) f[i] = u32x4{x[2 * i][0], x[2 * i][1], x[2 * i + 1][0], x[2 * i + 1][1]};
 }
 
-// A block's share: keys [begin, end) of a row for 16 * CT * W queries, of which each of the W waves has 16 * CT.  The waves share the keys' tiles.
-template <int D, bool F16, int CT, int W>
+// A block's share: keys [begin, end) of a row for 16 * CT * W queries.  V = 1: each of the W waves has 16 * CT of them, and the waves share the
+// keys' tiles.  W = 1: each of the V waves has all of them and keys of its own, and what the waves have is joined in LDS.
+template <int D, bool F16, int CT, int W, int V>
 struct Part {
+  static_assert(W == 1 || V == 1, "waves share keys or queries");
   static constexpr int SUB = W > 1 ? 2 : 1, KEYS = kTile * SUB;  // tiles, keys of a stage
   using E = Elem<F16>;
   static constexpr int CPR = D / 8, KK = D / 32, DT = D / 16;  // 16-byte pieces per key; products' steps; output tiles
@@ -118,6 +131,8 @@ struct Part {
 
   static __device__ __forceinline__ void run(const AttendArgs& a, const Plan& p, const Keys& ks, bool shared, int64_t row, int split, int tile0, u32x4* lds) {
     const int lane = threadIdx.x & 63, wave = W == 1 ? 0 : __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), col = lane & 15, quad = lane >> 4;
+    const int member = V == 1 ? 0 : __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    lds += member * (STAGES * STAGE);
     const int per = (int)(a.group * a.T), T = (int)a.T, M = (int)ks.m;
     const int b0 = tile0 * 16 * CT * W, m0 = b0 + wave * 16 * CT;
     const float c = kLog2e / __builtin_sqrtf((float)D);
@@ -138,7 +153,9 @@ struct Part {
       most = seen(len, T, one ? b1 % T : T - 1);
       least = seen(len, T, one ? b0 % T : 0);
     }
-    const int begin = split * ks.chunk, end = begin + ks.chunk < most ? begin + ks.chunk : most;
+    const int begin0 = split * ks.chunk, end0 = begin0 + ks.chunk < most ? begin0 + ks.chunk : most;
+    const int mine = V == 1 ? ks.chunk : (ks.chunk / V + kTile - 1) / kTile * kTile;
+    const int begin = begin0 + member * mine, end = begin + mine < end0 ? begin + mine : end0;
     const int n_stages = end > begin ? (end - begin + KEYS - 1) / KEYS : 0;
 
     float m_run[CT], l_run[CT];
@@ -353,14 +370,53 @@ struct Part {
       stages(full, n_stages, std::integral_constant<bool, true>{});
     }
     const size_t at = (size_t)(ks.first_split + split) * p.queries;
+    if constexpr (V == 1) {
 #pragma unroll
-    for (int ct = 0; ct < CT; ++ct) {
-      const float l = quads_sum(l_run[ct]);
-      if (m0 + ct * 16 + col < M) {
-        if (quad == 0) reinterpret_cast<float2*>(p.ml)[at + query[ct]] = float2{m_run[ct], l};
-        if (n_stages > 0) {
+      for (int ct = 0; ct < CT; ++ct) {
+        const float l = quads_sum(l_run[ct]);
+        if (m0 + ct * 16 + col < M) {
+          if (quad == 0) reinterpret_cast<float2*>(p.ml)[at + query[ct]] = float2{m_run[ct], l};
+          if (n_stages > 0) {
 #pragma unroll
-          for (int d = 0; d < DT; ++d) *reinterpret_cast<f32x4*>(p.o + (at + query[ct]) * D + d * 16 + quad * 4) = o[d][ct];
+            for (int d = 0; d < DT; ++d) *reinterpret_cast<f32x4*>(p.o + (at + query[ct]) * D + d * 16 + quad * 4) = o[d][ct];
+          }
+        }
+      }
+    } else {
+      // Every member's outputs by the largest reference, then their sum, in the members' order.
+      constexpr int Q = 16 * CT, LINE = D + 4;  // (a line's first bank differs from query to query)
+      static_assert(V * (Q * LINE + 2 * Q) * 4 <= V * STAGES * STAGE * 16, "the joined outputs lie where the stages were");
+      float* all = reinterpret_cast<float*>(lds - member * (STAGES * STAGE));
+      float2* ml = reinterpret_cast<float2*>(all + V * Q * LINE);
+      __syncthreads();  // everyone has read its last stage
+      float l_own[CT];
+#pragma unroll
+      for (int ct = 0; ct < CT; ++ct) {
+        l_own[ct] = quads_sum(l_run[ct]);
+        if (quad == 0) ml[member * Q + ct * 16 + col] = float2{m_run[ct], l_own[ct]};
+      }
+      __syncthreads();
+#pragma unroll
+      for (int ct = 0; ct < CT; ++ct) {
+        float m = kLow, l = 0.0f;
+#pragma unroll
+        for (int v = 0; v < V; ++v) m = __builtin_fmaxf(m, ml[v * Q + ct * 16 + col].x);
+#pragma unroll
+        for (int v = 0; v < V; ++v) l = __builtin_fmaf(ml[v * Q + ct * 16 + col].y, __builtin_amdgcn_exp2f(ml[v * Q + ct * 16 + col].x - m), l);
+        const float f = __builtin_amdgcn_exp2f(m_run[ct] - m);
+#pragma unroll
+        for (int d = 0; d < DT; ++d) *reinterpret_cast<f32x4*>(all + (member * Q + ct * 16 + col) * LINE + d * 16 + quad * 4) = o[d][ct] * f;
+        if (member == 0 && quad == 0 && m0 + ct * 16 + col < M) reinterpret_cast<float2*>(p.ml)[at + query[ct]] = float2{m, l};
+      }
+      __syncthreads();
+      if (end0 > begin0) {
+#pragma unroll
+        for (int i = 0; i < Q * D / 4 / (64 * V); ++i) {
+          const int x = i * 64 * V + threadIdx.x, q = x / (D / 4), d = x % (D / 4) * 4;
+          f32x4 sum = *reinterpret_cast<const f32x4*>(all + q * LINE + d);
+#pragma unroll
+          for (int v = 1; v < V; ++v) sum += *reinterpret_cast<const f32x4*>(all + (v * Q + q) * LINE + d);
+          if (m0 + q < M) *reinterpret_cast<f32x4*>(p.o + (at + query_at(shared, row, m0 + q, per, a.heads)) * D + d) = sum;
         }
       }
     }
@@ -373,52 +429,34 @@ __device__ __forceinline__ bool share_of(int b, const Keys& ks, int64_t& row, in
   const int64_t share = (int64_t)(b / (kXcds * ks.tiles)) * kXcds + b % kXcds;
   tile = b / kXcds % ks.tiles;
   row = share / ks.splits;
-  split = (int)(share % ks.splits);
+  // turned from row to row: with a number of shares that eight divides, one XCD would get every row's first, another every row's last, which
+  // rows that are not full do not have (256 rows of up to 8192 keys in 16 shares, 144 us, turned 132)
+  split = (int)((share + row) % ks.splits);
   return share < ks.rows * ks.splits;
 }
 
-// Few queries per row: a wave each.  CT: of the kind of keys that has the larger tiles.
-template <int D, bool F16, int CT>
-__global__ __launch_bounds__(64, CT == 1 ? 2 : 1) void attend_wave_kernel(AttendArgs a, Plan p) {
-  __shared__ u32x4 lds[Part<D, F16, CT, 1>::STAGES * Part<D, F16, CT, 1>::STAGE];
+// Few queries per row: V waves for a share of its keys.  CT: of the kind of keys that has the larger tiles.
+template <int D, bool F16, int CT, int V>
+__global__ __launch_bounds__(64 * V, CT == 1 ? 2 : 1) void attend_wave_kernel(AttendArgs a, Plan p) {
+  __shared__ u32x4 lds[V * Part<D, F16, CT, 1, V>::STAGES * Part<D, F16, CT, 1, V>::STAGE];
   const bool shared = (int)blockIdx.x < p.shared.blocks;
   const Keys& ks = shared ? p.shared : p.own;
   int64_t row;
   int split, tile;
   if (!share_of(shared ? blockIdx.x : blockIdx.x - p.shared.blocks, ks, row, split, tile)) return;
-  if (CT == 1 || ks.ct == 1) Part<D, F16, 1, 1>::run(a, p, ks, shared, row, split, tile, lds);
-  else Part<D, F16, CT, 1>::run(a, p, ks, shared, row, split, tile, lds);
+  if (CT == 1 || ks.ct == 1) Part<D, F16, 1, 1, V>::run(a, p, ks, shared, row, split, tile, lds);
+  else Part<D, F16, CT, 1, V>::run(a, p, ks, shared, row, split, tile, lds);
 }
 
 // Many: W waves of 32 queries share the keys.
 template <int D, bool F16, int W>
 __global__ __launch_bounds__(64 * W, W == 2 ? 1 : 2) void attend_block_kernel(AttendArgs a, Plan p, bool shared) {
-  __shared__ u32x4 lds[Part<D, F16, 2, W>::STAGES * Part<D, F16, 2, W>::STAGE];
+  __shared__ u32x4 lds[Part<D, F16, 2, W, 1>::STAGES * Part<D, F16, 2, W, 1>::STAGE];
   const Keys& ks = shared ? p.shared : p.own;
   int64_t row;
   int split, tile;
   if (!share_of(blockIdx.x, ks, row, split, tile)) return;
-  Part<D, F16, 2, W>::run(a, p, ks, shared, row, split, tile, lds);
-}
-
-// A query's shares, or some of them, put together: 2^m l is their sum, 2^m o their output.
-struct Joined {
-  float m, l;
-};
-__device__ __forceinline__ Joined join(const float* ml, int64_t query, int64_t queries, int splits, int lane) {  // by a wave
-  float m = kLow, l = 0.0f;
-  for (int s = lane; s < splits; s += 64) {
-    const float2 x = reinterpret_cast<const float2*>(ml)[(size_t)s * queries + query];
-    const float top = __builtin_fmaxf(m, x.x);
-    l = l * __builtin_amdgcn_exp2f(m - top) + x.y * __builtin_amdgcn_exp2f(x.x - top);
-    m = top;
-  }
-  for (int off = 32; off; off >>= 1) {
-    const float m2 = __shfl_xor(m, off, 64), l2 = __shfl_xor(l, off, 64), top = __builtin_fmaxf(m, m2);
-    l = l * __builtin_amdgcn_exp2f(m - top) + l2 * __builtin_amdgcn_exp2f(m2 - top);
-    m = top;
-  }
-  return {m, l};
+  Part<D, F16, 2, W, 1>::run(a, p, ks, shared, row, split, tile, lds);
 }
 
 // Joins the shares' outputs: D / 4 threads hold a share's row, so that a block takes 4 queries of few shares (QB = 4), or one query's
@@ -480,71 +518,125 @@ __device__ __forceinline__ void join_outputs(const AttendArgs& a, const Plan& p,
   }
 }
 
-// The account of 1024 keys of a row from logits that were kept, of up to MQ queries.
-template <int D, int MQ>
+// The account of 256 * KP keys of a row from logits that were kept, of up to MQ queries.
+template <int D, int MQ, int KP>
 __device__ __forceinline__ void account_kept(const AttendArgs& a, const Plan& p, const Keys& ks, bool shared, int b) {
+  typedef float keys_t __attribute__((ext_vector_type(KP)));
   __shared__ float lse[MQ];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, per = (int)(a.group * a.T), M = (int)ks.m, T = (int)a.T;
-  const int blocks = (int)((ks.n + 1023) / 1024), n = b % blocks * 1024 + threadIdx.x * 4;
+  const int per = (int)(a.group * a.T), M = (int)ks.m, T = (int)a.T;
+  const int blocks = (int)((ks.n + 256 * KP - 1) / (256 * KP)), n = b % blocks * (256 * KP) + threadIdx.x * KP;
   const int64_t row = b / blocks;
   const int len = row_len(shared ? a.shared_lens : a.lens, row, ks.n);
-  if (b % blocks * 1024 >= len) return;
+  if (b % blocks * (256 * KP) >= len) return;
   // (asked for before the joins: score rows have room for a whole quad)
-  const bool any = n < len;
-  f32x4 s[MQ];
+  keys_t s[MQ];
 #pragma unroll
   for (int m = 0; m < MQ; ++m)
-    s[m] = *reinterpret_cast<const f32x4*>(ks.scores + ((size_t)row * M + (m < M ? m : M - 1)) * ks.score_stride + (any ? n : 0));
+    s[m] = *reinterpret_cast<const keys_t*>(ks.scores + ((size_t)row * M + (m < M ? m : M - 1)) * ks.score_stride + (n < len ? n : 0));
   float* w = (shared ? a.weight_shared : a.weight) + row * ks.n;
-  f32x4 x;
+  float x[KP];
 #pragma unroll
-  for (int e = 0; e < 4; ++e) x[e] = w[n + e < len ? n + e : len - 1];
-  for (int m = wave; m < M; m += 4) {
-    const Joined j = join(p.ml, query_at(shared, row, m, per, a.heads), p.queries, p.splits, lane);
-    if (lane == 0) lse[m] = j.l == 0.0f ? -kNegInf : j.m + __builtin_amdgcn_logf(j.l);
+  for (int e = 0; e < KP; ++e) x[e] = w[n + e < len ? n + e : len - 1];
+  {  // 256 / MQ threads join a query's shares
+    constexpr int G = 256 / MQ;
+    const int m = threadIdx.x / G, g = threadIdx.x % G;
+    const int64_t query = query_at(shared, row, m < M ? m : M - 1, per, a.heads);
+    float top = kLow, l = 0.0f;
+#pragma unroll 4
+    for (int i = g; i < p.splits; i += G) {
+      const float2 y = reinterpret_cast<const float2*>(p.ml)[(size_t)i * p.queries + query];
+      const float t = __builtin_fmaxf(top, y.x);
+      l = l * __builtin_amdgcn_exp2f(top - t) + y.y * __builtin_amdgcn_exp2f(y.x - t);
+      top = t;
+    }
+#pragma unroll
+    for (int off = G / 2; off; off >>= 1) {
+      const float m2 = __shfl_xor(top, off, 64), l2 = __shfl_xor(l, off, 64), t = __builtin_fmaxf(top, m2);
+      l = l * __builtin_amdgcn_exp2f(top - t) + l2 * __builtin_amdgcn_exp2f(m2 - t);
+      top = t;
+    }
+    if (g == 0) lse[m] = m >= M || l == 0.0f ? -kNegInf : top + __builtin_amdgcn_logf(l);
   }
   __syncthreads();
   const float c = kLog2e / __builtin_sqrtf((float)D);
-  f32x4 sum = {0, 0, 0, 0};
+  float sum[KP] = {};
 #pragma unroll
   for (int m = 0; m < MQ; ++m) {
-    const float ref = m < M ? lse[m] : -kNegInf;
+    const float ref = lse[m];
     const int see = m < M ? shared ? len : seen(len, T, m % T) : 0;
 #pragma unroll
-    for (int e = 0; e < 4; ++e) sum[e] += n + e < see ? __builtin_amdgcn_exp2f(__builtin_fmaf(s[m][e], c, -ref)) : 0.0f;
+    for (int e = 0; e < KP; ++e) sum[e] += n + e < see ? __builtin_amdgcn_exp2f(__builtin_fmaf(s[m][e], c, -ref)) : 0.0f;
   }
 #pragma unroll
-  for (int e = 0; e < 4; ++e)
+  for (int e = 0; e < KP; ++e)
     if (n + e < len) w[n + e] = x[e] + sum[e];
 }
 
 // Blocks below `query_blocks` join outputs, those behind them keep the account.
-template <int D, bool F16, int QB, int MQ>
+template <int D, bool F16, int QB, int MQ, int KP>
 __global__ __launch_bounds__(256) void attend_finish_kernel(AttendArgs a, Plan p, int query_blocks, int shared_blocks) {
   const int b = (int)blockIdx.x - query_blocks;
   if (b < 0) return join_outputs<D, F16, QB>(a, p, blockIdx.x);
   if constexpr (MQ > 0) {
     const bool shared = b < shared_blocks;
-    account_kept<D, MQ>(a, p, shared ? p.shared : p.own, shared, shared ? b : b - shared_blocks);
+    account_kept<D, MQ, KP>(a, p, shared ? p.shared : p.own, shared, shared ? b : b - shared_blocks);
   }
 }
 
-// The account where the logits were not kept: a block takes 128 keys of a row and walks the queries that see them, 64 at a time, which all
-// its waves have in LDS: two waves take 64 keys each with one half of those, two with the other.  S: a lane has the logits of its
-// key (column) with queries 4 quad + r, so that a key's sum stays in the lane until the end.  The products of the next 16 queries are
-// spread between the exponentials of the 16 before: one after the other, matrix and vector instructions of a SIMD's waves take turns.
+// The account where the logits were not kept: a block takes 256 keys of a row, 64 in each wave's registers, and walks the queries that see
+// them, or one of `parts` parts of those, 64 at a time, through LDS.  S: a lane has the logits of its key (column) with queries 4 quad + r, so
+// that a key's sum stays in the lane until the end.  The products of 16 queries are spread between the exponentials of the 16 before: one
+// after the other, matrix and vector instructions of a SIMD's waves take turns.  Sums of parts are added up by attend_add_kernel.
 template <int D, bool F16>
-__global__ __launch_bounds__(256, 2) void attend_account_kernel(AttendArgs a, Keys ks, bool shared, const float* __restrict__ lse) {
+__global__ __launch_bounds__(256, 2) void attend_account_kernel(AttendArgs a, Keys ks, bool shared, const float* __restrict__ lse, int parts,
+                                                                float* __restrict__ part_sums) {
   using E = Elem<F16>;
   constexpr int CPR = D / 8, KK = D / 32, QS = 64, STAGE = QS * CPR + QS / 4, LOADS = QS * CPR / 256;  // queries, 16-byte units and a wave's loads of a step
   __shared__ u32x4 lds[3 * STAGE];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), col = lane & 15, quad = lane >> 4;
-  const int per = (int)(a.group * a.T), T = (int)a.T, M = (int)ks.m, blocks = (int)((ks.n + 127) / 128);
-  const int64_t row = blockIdx.x / blocks;
-  const int b0 = blockIdx.x % blocks * 128, n0 = b0 + (wave & 1) * 64, half = wave >> 1;
+  const int per = (int)(a.group * a.T), T = (int)a.T, M = (int)ks.m, blocks = (int)((ks.n + 255) / 256);
+  // a row's last keys first: those that only some queries see take longest
+  const int rows = (int)ks.rows, part = blockIdx.x % parts, b0 = (blocks - 1 - (int)(blockIdx.x / parts / rows)) * 256, n0 = b0 + wave * 64;
+  const int64_t row = blockIdx.x / parts % rows;
+  const float inv_T = 1.0f / (float)T;
   const int len = row_len(shared ? a.shared_lens : a.lens, row, ks.n);
   if (b0 >= len) return;
+  const int all = (M + QS - 1) / QS, first = (int)((int64_t)all * part / parts), steps = (int)((int64_t)all * (part + 1) / parts) - first;  // (parts <= all)
   const float c = kLog2e / __builtin_sqrtf((float)D);
+  typedef const __attribute__((address_space(1))) void* gptr_t;
+  typedef __attribute__((address_space(3))) void* lptr_t;
+  // This lane's pieces of a step: query r of it, whose row in q moves on by QS queries: a whole number of sequences and `turn` queries of the next.
+  const int heads = shared ? (int)a.heads : 1, each = shared ? per : M;
+  const uint8_t* qb = (const uint8_t*)a.q + (size_t)row * each * (D * 2);
+  uint32_t at[LOADS];
+  int of[LOADS];  // which of its sequence's queries
+#pragma unroll
+  for (int i = 0; i < LOADS; ++i) {
+    const int r = (i * 4 + wave) * (64 / CPR) + lane / CPR, m = first * QS + r < M ? first * QS + r : M - 1;
+    of[i] = m % each;
+    at[i] = (uint32_t)(((m / each) * heads * each + of[i]) * (D * 2) + ((lane % CPR) ^ swizzle<D>(r)) * 16);
+  }
+  const int turn = QS % each, on = (QS / each * heads * each + turn) * (D * 2), wrap = (heads - 1) * each * (D * 2);
+  int fetched = first;
+  auto fetch = [&](int stage) __attribute__((always_inline)) {  // the next step
+    u32x4* st = lds + stage * STAGE;
+    const int left = M - 1 - fetched * QS;
+#pragma unroll
+    for (int i = 0; i < LOADS; ++i) {
+      __builtin_amdgcn_global_load_lds((gptr_t)(qb + at[i]), (lptr_t)(st + (i * 4 + wave) * 64), 16, 0, 0);
+      const int r = (i * 4 + wave) * (64 / CPR) + lane / CPR;
+      if (r + QS <= left) {  // (a query behind the last: the same row again, which counts nowhere)
+        of[i] += turn;
+        const bool over = of[i] >= each;
+        of[i] -= over ? each : 0;
+        at[i] += (uint32_t)(on + (over ? wrap : 0));
+      }
+    }
+    // every wave, so that all have as many loads under way
+    const int m = fetched * QS + lane < M ? fetched * QS + lane : M - 1;
+    __builtin_amdgcn_global_load_lds((gptr_t)(lse + row * M + m), (lptr_t)(st + QS * CPR), 4, 0, 0);
+    ++fetched;
+  };
   u32x4 bk[4][KK];
 #pragma unroll
   for (int kt = 0; kt < 4; ++kt) {
@@ -553,30 +645,14 @@ __global__ __launch_bounds__(256, 2) void attend_account_kernel(AttendArgs a, Ke
 #pragma unroll
     for (int kk = 0; kk < KK; ++kk) bk[kt][kk] = *reinterpret_cast<const u32x4*>(k + kk * 32);
   }
-  typedef const __attribute__((address_space(1))) void* gptr_t;
-  typedef __attribute__((address_space(3))) void* lptr_t;
-  const int steps = (M + QS - 1) / QS;
-  auto fetch = [&](int t, int stage) __attribute__((always_inline)) {
-    u32x4* st = lds + stage * STAGE;
-#pragma unroll
-    for (int i = 0; i < LOADS; ++i) {
-      const int j = wave * LOADS + i, r = j * (64 / CPR) + lane / CPR, m = t * QS + r < M ? t * QS + r : M - 1;
-      const uint16_t* q = (const uint16_t*)a.q + query_at(shared, row, m, per, a.heads) * D + ((lane % CPR) ^ swizzle<D>(r)) * 8;
-      __builtin_amdgcn_global_load_lds((gptr_t)q, (lptr_t)(st + j * 64), 16, 0, 0);
-    }
-    // every wave, so that all have as many loads under way
-    const int m = t * QS + lane < M ? t * QS + lane : M - 1;
-    __builtin_amdgcn_global_load_lds((gptr_t)(lse + row * M + m), (lptr_t)(st + QS * CPR), 4, 0, 0);
-  };
   struct Logits {
     f32x4 s[4], ref;
   };
   float sum[4] = {};
-  auto read = [&](u32x4 (&fq)[KK], Logits& x, const u32x4* st, int rt) __attribute__((always_inline)) {
-    const int r0 = half * (QS / 2) + rt * 16, r = r0 + col;
+  auto read = [&](u32x4 (&fq)[KK], const u32x4* st, int u) __attribute__((always_inline)) {
+    const int r = u * 16 + col;
 #pragma unroll
     for (int kk = 0; kk < KK; ++kk) fq[kk] = st[r * CPR + ((kk * 4 + quad) ^ swizzle<D>(r))];
-    x.ref = reinterpret_cast<const f32x4*>(st + QS * CPR)[r0 / 4 + quad];
   };
   auto products = [&](const u32x4 (&fq)[KK], Logits& x) __attribute__((always_inline)) {
 #pragma unroll
@@ -592,118 +668,149 @@ __global__ __launch_bounds__(256, 2) void attend_account_kernel(AttendArgs a, Ke
 #pragma unroll
       for (int e = 0; e < 4; ++e) sum[kt] += __builtin_amdgcn_exp2f(__builtin_fmaf(x.s[kt][e], c, -x.ref[e]));
   };
-  auto add_cut = [&](const Logits& x, int q0, int rt) __attribute__((always_inline)) {
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      const int m = q0 + half * (QS / 2) + rt * 16 + quad * 4 + e, see = m >= M ? 0 : shared ? len : seen(len, T, m % T);
-#pragma unroll
-      for (int kt = 0; kt < 4; ++kt) {
-        const float y = __builtin_amdgcn_exp2f(__builtin_fmaf(x.s[kt][e], c, -x.ref[e]));
-        sum[kt] += n0 + kt * 16 + col < see ? y : 0.0f;
-      }
-    }
-  };
   // waits until this wave's part of step t has landed
   auto landed = [&](int t) __attribute__((always_inline)) {
     __builtin_amdgcn_s_waitcnt(0x0F70 | (LOADS + 1));  // (on every path: it is where the compiler knows of the keys)
     if (t + 1 >= steps) __builtin_amdgcn_s_waitcnt(0x0F70);
     asm volatile("" ::: "memory");
   };
-  fetch(0, 0);
-  if (steps > 1) fetch(1, 1);
+  fetch(0);
+  if (steps > 1) fetch(1);
   landed(0);  // and with it the resident keys: where the compiler does not know, it waits for all loads in front of every step's products
-  // Logits that wait for their exponentials go from one step to the next: none at first, which a reference of +infinity makes zeros of.
-  Logits pending;
-#pragma unroll
-  for (int kt = 0; kt < 4; ++kt) pending.s[kt] = f32x4{0, 0, 0, 0};
-  pending.ref = f32x4{-kNegInf, -kNegInf, -kNegInf, -kNegInf};
   int stage = 0;
   for (int t = 0; t < steps; ++t) {
     landed(t);
     __builtin_amdgcn_s_barrier();  // everyone's has, and everyone has read step t - 1, whose place takes step t + 2
     asm volatile("" ::: "memory");
-    if (t + 2 < steps) fetch(t + 2, stage == 0 ? 2 : stage - 1);
+    if (t + 2 < steps) fetch(stage == 0 ? 2 : stage - 1);
     const u32x4* st = lds + stage * STAGE;
+    const f32x4* refs = reinterpret_cast<const f32x4*>(st + QS * CPR) + quad;
     // whether all the step's queries see all of this wave's keys
-    const int q0 = t * QS, q1 = q0 + QS - 1;
-    const int least = shared ? len : seen(len, T, q0 / T == q1 / T ? q0 % T : 0);
-    if (q1 < M && n0 + 64 <= least) {
-      static_for<QS / 32>([&](auto rt) __attribute__((always_inline)) {
-        u32x4 fq[KK];
-        Logits next;
-        read(fq, next, st, decltype(rt)::value);
-        __builtin_amdgcn_sched_barrier(0);
-        products(fq, next);
-        add(pending);
-#pragma unroll
-        for (int i = 0; i < 4 * KK; ++i) {
-          __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);             // one product
-          __builtin_amdgcn_sched_group_barrier(0x002, 48 / (4 * KK), 0);  // its share of 16 fma, 16 exponentials and 16 additions
+    const int q0 = (first + t) * QS, q1 = q0 + QS - 1;
+    const int t0 = shared ? 0 : q0 % T;
+    const int least = shared ? len : seen(len, T, t0 + QS <= T ? t0 : 0);
+    auto work = [&](auto cut_c) __attribute__((always_inline)) {
+      constexpr bool cut = decltype(cut_c)::value;
+      u32x4 fq[2][KK];
+      Logits x[2];
+      read(fq[0], st, 0);
+      read(fq[1], st, 1);
+      x[0].ref = refs[0];
+      products(fq[0], x[0]);
+      static_for<4>([&](auto uc) __attribute__((always_inline)) {
+        constexpr int u = decltype(uc)::value, cur = u & 1, nxt = cur ^ 1;
+        if constexpr (u < 3) {
+          x[nxt].ref = refs[(u + 1) * 4];
+          if constexpr (u < 2) read(fq[cur], st, u + 2);
+          if constexpr (!cut) __builtin_amdgcn_sched_barrier(0);
+          products(fq[nxt], x[nxt]);
         }
-        __builtin_amdgcn_sched_barrier(0);
-        pending = next;
+        if constexpr (cut) {
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const int m = q0 + u * 16 + quad * 4 + e, see = m >= M ? 0 : shared ? len : seen(len, T, remainder_of(m, T, inv_T));
+#pragma unroll
+            for (int kt = 0; kt < 4; ++kt) {
+              const float y = __builtin_amdgcn_exp2f(__builtin_fmaf(x[cur].s[kt][e], c, -x[cur].ref[e]));
+              sum[kt] += n0 + kt * 16 + col < see ? y : 0.0f;
+            }
+          }
+        } else {
+          add(x[cur]);
+          if constexpr (u < 3) {
+#pragma unroll
+            for (int i = 0; i < 4 * KK; ++i) {
+              __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);              // one product
+              __builtin_amdgcn_sched_group_barrier(0x002, 48 / (4 * KK), 0);  // its share of 16 fma, 16 exponentials and 16 additions
+            }
+            __builtin_amdgcn_sched_barrier(0);
+          }
+        }
       });
-    } else {
-      static_for<QS / 32>([&](auto rt) __attribute__((always_inline)) {
-        u32x4 fq[KK];
-        Logits next;
-        read(fq, next, st, decltype(rt)::value);
-        products(fq, next);
-        add_cut(next, q0, decltype(rt)::value);
-      });
-    }
+    };
+    const int any = shared ? len : seen(len, T, t0 + QS <= T ? t0 + QS - 1 : T - 1);  // keys that some of the step's queries see
+    if (__builtin_expect(q1 < M && n0 + 64 <= least, 1)) work(std::integral_constant<bool, false>{});
+    else if (n0 < any) work(std::integral_constant<bool, true>{});
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
     stage = stage == 2 ? 0 : stage + 1;
   }
-  add(pending);
-  __syncthreads();
   float* w = (shared ? a.weight_shared : a.weight) + row * ks.n;
-  float* other = reinterpret_cast<float*>(lds);
+  float* mine = part_sums + ((size_t)part * ks.rows + row) * ks.n;
 #pragma unroll
-  for (int kt = 0; kt < 4; ++kt) sum[kt] = quads_sum(sum[kt]);
-  if (half == 1 && quad == 0) {
-#pragma unroll
-    for (int kt = 0; kt < 4; ++kt) other[(wave & 1) * 64 + kt * 16 + col] = sum[kt];
-  }
-  __syncthreads();
-  if (half == 0 && quad == 0) {
-#pragma unroll
-    for (int kt = 0; kt < 4; ++kt) {
-      const int n = n0 + kt * 16 + col;
-      if (n < len) w[n] += sum[kt] + other[(wave & 1) * 64 + kt * 16 + col];
+  for (int kt = 0; kt < 4; ++kt) {
+    const int n = n0 + kt * 16 + col;
+    const float x = quads_sum(sum[kt]);
+    if (quad == 0 && n < len) {
+      if (parts > 1) mine[n] = x;
+      else w[n] += x;
     }
   }
 }
 
-// Shares of at least kLeastKeys keys, as many as give the chip kWaves waves of this kind.
-#ifndef PKV_LEAST
-#define PKV_LEAST 128
-#endif
-#ifndef PKV_WAVES
-#define PKV_WAVES 2048
-#endif
-constexpr int64_t kLeastKeys = PKV_LEAST, kWaves = PKV_WAVES, kMostSplits = 512;
+__global__ __launch_bounds__(256) void attend_add_kernel(float* __restrict__ weight, const float* __restrict__ part_sums, const int32_t* __restrict__ lens,
+                                                         int64_t rows, int64_t n, int parts) {
+  const int blocks = (int)((n + 255) / 256);
+  const int64_t row = blockIdx.x / blocks;
+  const int i = blockIdx.x % blocks * 256 + threadIdx.x;
+  if (i >= row_len(lens, row, n)) return;
+  float x = 0.0f;
+  for (int p = 0; p < parts; ++p) x += part_sums[((size_t)p * rows + row) * n + i];
+  weight[row * n + i] += x;
+}
 
-Keys keys_of(int64_t rows, int64_t n, int64_t m, bool account) {
+// Parts of the queries in attend_account_kernel: where a row's keys are few blocks, the last turn on the compute units is mostly empty.
+int account_parts(const Keys& k) {
+  const int64_t blocks = k.rows * ((k.n + 255) / 256), steps = (k.m + 63) / 64;
+  int best = 1;
+  double least = 1e30;
+  for (int p = 1; p <= 8 && p <= steps; ++p) {
+    const double turns = (double)((blocks * p + 255) / 256) * (double)((steps + p - 1) / p) + 1.0 * p;
+    if (turns < least) {
+      least = turns;
+      best = p;
+    }
+  }
+  return best;
+}
+
+constexpr int kMerge = 4;
+constexpr int64_t kMostSplits = 512;
+
+Keys keys_of(int64_t rows, int64_t n, int64_t m, int merge, bool account) {
   Keys k = {};
   k.rows = rows;
   k.n = n;
   k.m = m;
+  k.merge = 1;
   if (n == 0) {
     k.tiles = 1;
     return k;
   }
   k.ct = m <= 16 ? 1 : 2;
   k.waves = m <= 32 ? 1 : m <= 64 ? 2 : m <= 128 ? 4 : 8;
-  const int64_t tile = 16 * k.ct * k.waves;
+  if (k.waves == 1) k.merge = merge;
+  const int64_t tile = 16 * k.ct * k.waves, jobs = rows * ((m + tile - 1) / tile);
   k.tiles = (int)((m + tile - 1) / tile);
-  int64_t splits = (kWaves + rows * k.tiles * k.waves - 1) / (rows * k.tiles * k.waves);
-  const int64_t most = (n + kLeastKeys - 1) / kLeastKeys;
+  int64_t splits, least;
+  if (k.waves > 1) {
+    splits = (2048 / k.waves + jobs - 1) / jobs;
+    least = 256;
+  } else if (k.merge > 1) {
+    splits = (n + 511) / 512;
+    if (jobs * splits < 256) splits = (256 + jobs - 1) / jobs;
+    least = 256;
+  } else {
+    least = jobs * n <= 64 * 256 ? 64 : jobs * n <= 128 * 1024 ? 128 : PKV_BIG;
+    splits = kMostSplits;
+  }
+  const int64_t most = (n + least - 1) / least;
   splits = splits < most ? splits : most;
   splits = splits < kMostSplits ? splits : kMostSplits;
-  k.chunk = (int)(((n + splits - 1) / splits + kTile - 1) / kTile * kTile);
+  const int64_t step = kTile * k.merge;
+  k.chunk = (int)(((n + splits - 1) / splits + step - 1) / step * step);
   k.splits = (int)((n + k.chunk - 1) / k.chunk);
   k.blocks = (int)((rows * k.splits + kXcds - 1) / kXcds * kXcds * k.tiles);
+  k.parts = account && m > kKeptQueries ? account_parts(k) : 1;
   k.score_stride = account && m <= kKeptQueries ? (n + kTile - 1) / kTile * kTile : 0;
   return k;
 }
@@ -712,8 +819,11 @@ size_t plan_of(const AttendArgs& a, Plan* out, uint8_t* scratch) {
   const int64_t per = a.group * a.T, rows = a.batch * a.heads;
   Plan p = {};
   p.queries = rows * per;
-  p.shared = keys_of(a.heads, a.P, a.batch * per, a.weight_shared != nullptr);
-  p.own = keys_of(rows, a.N, per, a.weight != nullptr);
+  const int64_t m_shared = a.P > 0 ? a.batch * per : 0, m_own = a.N > 0 ? per : 0;
+  // waves are joined in LDS where they leave outputs of more than 16 queries: those would be a quarter of what is read
+  const int merge = (m_shared > 16 && m_shared <= 32) || (m_own > 16 && m_own <= 32) ? kMerge : 1;
+  p.shared = keys_of(a.heads, a.P, a.batch * per, merge, a.weight_shared != nullptr);
+  p.own = keys_of(rows, a.N, per, merge, a.weight != nullptr);
   p.own.first_split = p.shared.splits;
   p.splits = p.shared.splits + p.own.splits;
   size_t at = 0;
@@ -725,6 +835,9 @@ size_t plan_of(const AttendArgs& a, Plan* out, uint8_t* scratch) {
   p.ml = take((size_t)p.splits * p.queries * 2);
   p.o = take((size_t)p.splits * p.queries * a.D);
   p.lse = take((size_t)p.queries * 2);
+  const size_t sums_shared = p.shared.parts > 1 ? (size_t)(p.shared.parts * p.shared.rows * p.shared.n) : 0;
+  const size_t sums_own = p.own.parts > 1 ? (size_t)(p.own.parts * p.own.rows * p.own.n) : 0;
+  p.part_sums = take(sums_shared > sums_own ? sums_shared : sums_own);
   if (p.shared.score_stride) p.shared.scores = take((size_t)(p.shared.rows * p.shared.m * p.shared.score_stride));
   if (p.own.score_stride) p.own.scores = take((size_t)(p.own.rows * p.own.m * p.own.score_stride));
   if (out) *out = p;
@@ -750,36 +863,46 @@ hipError_t launch_attend_of(const AttendArgs& a, void* scratch, hipStream_t stre
   if (p.own.waves > 1) few.own.blocks = 0;
   const unsigned blocks = (unsigned)(few.shared.blocks + few.own.blocks);
   if (e == hipSuccess && blocks > 0) {
-    if ((few.shared.blocks && p.shared.ct == 2) || (few.own.blocks && p.own.ct == 2)) attend_wave_kernel<D, F16, 2><<<blocks, 64, 0, stream>>>(a, few);
-    else attend_wave_kernel<D, F16, 1><<<blocks, 64, 0, stream>>>(a, few);
+    if (p.shared.merge > 1 || p.own.merge > 1) attend_wave_kernel<D, F16, 2, kMerge><<<blocks, 64 * kMerge, 0, stream>>>(a, few);
+    else attend_wave_kernel<D, F16, 1, 1><<<blocks, 64, 0, stream>>>(a, few);
     e = hipGetLastError();
   }
   if (e != hipSuccess) return e;
-  const int64_t shared_blocks = p.shared.scores ? p.shared.rows * ((p.shared.n + 1023) / 1024) : 0;
-  const int64_t own_blocks = p.own.scores ? p.own.rows * ((p.own.n + 1023) / 1024) : 0;
   const int64_t kept_shared = p.shared.scores ? p.shared.m : 0, kept_own = p.own.scores ? p.own.m : 0, kept = kept_shared > kept_own ? kept_shared : kept_own;
-  auto finish = [&](auto qb, auto mq) {
-    constexpr int QB = decltype(qb)::value, MQ = decltype(mq)::value;
+  const int64_t kept_keys = (p.shared.scores ? p.shared.rows * p.shared.n : 0) + (p.own.scores ? p.own.rows * p.own.n : 0);
+  auto finish = [&](auto qb, auto mq, auto kp) {
+    constexpr int QB = decltype(qb)::value, MQ = decltype(mq)::value, KP = decltype(kp)::value;
     const int query_blocks = (int)((p.queries + QB - 1) / QB);
-    attend_finish_kernel<D, F16, QB, MQ><<<(unsigned)(query_blocks + shared_blocks + own_blocks), 256, 0, stream>>>(a, p, query_blocks, (int)shared_blocks);
+    auto key_blocks = [&](const Keys& k) { return k.scores ? k.rows * ((k.n + 256 * KP - 1) / (256 * KP)) : 0; };
+    const int64_t shared_blocks = key_blocks(p.shared), own_blocks = key_blocks(p.own);
+    attend_finish_kernel<D, F16, QB, MQ, KP><<<(unsigned)(query_blocks + shared_blocks + own_blocks), 256, 0, stream>>>(a, p, query_blocks, (int)shared_blocks);
   };
   auto finish_of = [&](auto qb) {
-    if (kept == 0) finish(qb, std::integral_constant<int, 0>{});
-    else if (kept <= 4) finish(qb, std::integral_constant<int, 4>{});
-    else if (kept <= 8) finish(qb, std::integral_constant<int, 8>{});
-    else finish(qb, std::integral_constant<int, 16>{});
+    auto with = [&](auto mq) {  // four keys a thread where that still gives every compute unit two blocks
+      if (kept_keys >= 512 * 1024) finish(qb, mq, std::integral_constant<int, 4>{});
+      else finish(qb, mq, std::integral_constant<int, 1>{});
+    };
+    if (kept == 0) finish(qb, std::integral_constant<int, 0>{}, std::integral_constant<int, 1>{});
+    else if (kept <= 4) with(std::integral_constant<int, 4>{});
+    else if (kept <= 8) with(std::integral_constant<int, 8>{});
+    else if (kept <= 16) with(std::integral_constant<int, 16>{});
+    else with(std::integral_constant<int, 32>{});
   };
   if (p.splits <= 8) finish_of(std::integral_constant<int, 4>{});
   else finish_of(std::integral_constant<int, 1>{});
   e = hipGetLastError();
-  if (e == hipSuccess && a.weight_shared != nullptr && !p.shared.scores) {
-    attend_account_kernel<D, F16><<<(unsigned)(p.shared.rows * ((p.shared.n + 127) / 128)), 256, 0, stream>>>(a, p.shared, true, p.lse + p.queries);
+  auto account = [&](const Keys& k, bool shared, float* weight, const int32_t* lens, const float* lse) {
+    if (e != hipSuccess || weight == nullptr || k.n == 0 || k.scores) return;
+    const int64_t blocks = k.rows * ((k.n + 255) / 256);
+    attend_account_kernel<D, F16><<<(unsigned)(blocks * k.parts), 256, 0, stream>>>(a, k, shared, lse, k.parts, p.part_sums);
     e = hipGetLastError();
-  }
-  if (e == hipSuccess && a.weight != nullptr && p.own.n > 0 && !p.own.scores) {
-    attend_account_kernel<D, F16><<<(unsigned)(p.own.rows * ((p.own.n + 127) / 128)), 256, 0, stream>>>(a, p.own, false, p.lse);
-    e = hipGetLastError();
-  }
+    if (e == hipSuccess && k.parts > 1) {
+      attend_add_kernel<<<(unsigned)blocks, 256, 0, stream>>>(weight, p.part_sums, lens, k.rows, k.n, k.parts);
+      e = hipGetLastError();
+    }
+  };
+  account(p.shared, true, a.weight_shared, a.shared_lens, p.lse + p.queries);
+  account(p.own, false, a.weight, a.lens, p.lse);
   return e;
 }
 
