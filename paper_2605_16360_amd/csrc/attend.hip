@@ -34,21 +34,21 @@ struct Elem {
     if constexpr (F16) return mfma_f16_16x16x32(as_f16x8(a), as_f16x8(b), c);
     else return mfma_bf16_16x16x32(as_bf16x8(a), as_bf16x8(b), c);
   }
-  // p as the sums of two 16-bit values: the second holds what the first leaves
-  static __device__ __forceinline__ u32x2 split(float p0, float p1) {
-    uint32_t hi, lo;
-    typedef float f32x2 __attribute__((ext_vector_type(2)));
-    typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
-    typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+  // Two probabilities as sums of two 16-bit values each: rounded, and what that leaves.
+  typedef float f32x2 __attribute__((ext_vector_type(2)));
+  typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
+  typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+  static __device__ __forceinline__ uint32_t first(float p0, float p1) {
+    if constexpr (F16) return __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2{p0, p1}), f16x2));
+    else return __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2{p0, p1}), bf16x2));
+  }
+  static __device__ __forceinline__ uint32_t rest(float p0, float p1, uint32_t hi) {
     if constexpr (F16) {
-      const f16x2 h = __builtin_convertvector((f32x2{p0, p1}), f16x2);
-      hi = __builtin_bit_cast(uint32_t, h);
-      lo = __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2{p0 - (float)h[0], p1 - (float)h[1]}), f16x2));
+      const f16x2 h = __builtin_bit_cast(f16x2, hi);
+      return first(p0 - (float)h[0], p1 - (float)h[1]);
     } else {
-      hi = __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2{p0, p1}), bf16x2));
-      lo = __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2{p0 - __uint_as_float(hi << 16), p1 - __uint_as_float(hi & 0xffff0000u)}), bf16x2));
+      return first(p0 - __uint_as_float(hi << 16), p1 - __uint_as_float(hi & 0xffff0000u));
     }
-    return {hi, lo};
   }
 };
 
@@ -125,7 +125,8 @@ struct Part {
   using E = Elem<F16>;
   static constexpr int CPR = D / 8, KK = D / 32, DT = D / 16;  // 16-byte pieces per key; products' steps; output tiles
   static constexpr int NL = KEYS * CPR / 64;                   // a stage's loads of K, by a wave
-  static constexpr int STAGES = 2, STAGE = 2 * NL * 64;
+  static constexpr bool PIPE = W == 8;  // products a tile ahead of their exponentials
+  static constexpr int STAGES = PIPE ? 3 : 2, STAGE = 2 * NL * 64;
   static constexpr int MINE = 2 * NL / W;                      // loads of a wave per stage
   static_assert(MINE * W == 2 * NL, "the waves share a stage's loads");
 
@@ -191,24 +192,72 @@ struct Part {
           __builtin_amdgcn_global_load_lds((gptr_t)(vt + at), (lptr_t)(st + (NL + i * W) * 64), 16, 0, 0);
         });
       };
-      auto tile = [&](int n0, const u32x4* st, auto cut_c) __attribute__((always_inline)) {  // keys from n0 on
-        constexpr bool cut = decltype(cut_c)::value;
-        // S^T: a lane has the logits of its query (column) with keys 4 quad + r and 16 + 4 quad + r
-        f32x4 s[2][CT];
+      // S^T of a tile: a lane has the logits of its query (column) with keys 4 quad + r and 16 + 4 quad + r
+      auto read_k = [&](const u32x4* st, u32x4 (&f)[2][KK]) __attribute__((always_inline)) {
 #pragma unroll
-        for (int kt = 0; kt < 2; ++kt) {
-          u32x4 f[KK];
+        for (int kt = 0; kt < 2; ++kt)
 #pragma unroll
           for (int kk = 0; kk < KK; ++kk) {
             const int r = kt * 16 + col;
-            f[kk] = st[r * CPR + ((kk * 4 + quad) ^ swizzle<D>(r))];
+            f[kt][kk] = st[r * CPR + ((kk * 4 + quad) ^ swizzle<D>(r))];
           }
+      };
+      auto logits = [&](const u32x4 (&f)[2][KK], f32x4 (&s)[2][CT]) __attribute__((always_inline)) {
+#pragma unroll
+        for (int kt = 0; kt < 2; ++kt)
 #pragma unroll
           for (int ct = 0; ct < CT; ++ct) s[kt][ct] = f32x4{0, 0, 0, 0};
 #pragma unroll
-          for (int kk = 0; kk < KK; ++kk)
+        for (int kk = 0; kk < KK; ++kk)
 #pragma unroll
-            for (int ct = 0; ct < CT; ++ct) s[kt][ct] = E::mfma(f[kk], bq[ct][kk], s[kt][ct]);
+          for (int kt = 0; kt < 2; ++kt)
+#pragma unroll
+            for (int ct = 0; ct < CT; ++ct) s[kt][ct] = E::mfma(f[kt][kk], bq[ct][kk], s[kt][ct]);
+      };
+      // Probabilities by the reference that there is; only where some of a lane's come to more than kMostSum are the logits' maxima taken, the
+      // reference moved and the probabilities computed again (at first always).
+      auto probabilities = [&](const f32x4 (&s)[2][CT], int ct, float (&pf)[8]) __attribute__((always_inline)) {
+        float sum = 0.0f;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          pf[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[i >> 2][ct][i & 3], c, -m_run[ct]));
+          sum += pf[i];
+        }
+        return sum;
+      };
+      auto keep_reference = [&](const f32x4 (&s)[2][CT], float (&pf)[CT][8], float (&sum)[CT]) __attribute__((always_inline)) {
+        bool much = false;
+#pragma unroll
+        for (int ct = 0; ct < CT; ++ct) much = much || !(sum[ct] <= kMostSum);
+        if (__builtin_expect(__builtin_amdgcn_ballot_w64(much) != 0, 0)) {
+#pragma unroll
+          for (int ct = 0; ct < CT; ++ct) {
+            float top = max3f(s[0][ct][0], s[0][ct][1], s[0][ct][2]);
+            top = max3f(top, s[0][ct][3], s[1][ct][0]);
+            top = max3f(top, s[1][ct][1], s[1][ct][2]);
+            top = quads_max(__builtin_fmaxf(top, s[1][ct][3])) * c;
+            const float m = __builtin_fmaxf(m_run[ct], top), f = __builtin_amdgcn_exp2f(m_run[ct] - m);
+            m_run[ct] = m;
+            l_run[ct] *= f;
+#pragma unroll
+            for (int d = 0; d < DT; ++d) o[d][ct] *= f;
+            sum[ct] = probabilities(s, ct, pf[ct]);
+          }
+        }
+#pragma unroll
+        for (int ct = 0; ct < CT; ++ct) l_run[ct] += sum[ct];
+      };
+      auto place_v = [&](const u32x4* vst) __attribute__((always_inline)) {  // this lane's piece of the first transposed fragment
+        const int vr = quad * 4 + (col >> 2);
+        return (uint32_t)(uintptr_t)(__attribute__((address_space(3))) const void*)(vst + vr * CPR + (((col >> 1) & 1) ^ swizzle<D>(vr))) + (col & 1) * 8;
+      };
+      auto tile = [&](int n0, const u32x4* st, auto cut_c) __attribute__((always_inline)) {  // keys from n0 on
+        constexpr bool cut = decltype(cut_c)::value;
+        f32x4 s[2][CT];
+        {
+          u32x4 f[2][KK];
+          read_k(st, f);
+          logits(f, s);
         }
         if (W == 1 && ks.scores != nullptr) {
 #pragma unroll
@@ -222,51 +271,26 @@ struct Part {
           }
         }
         u32x4 hi[CT], lo[CT];
-        float pf[CT][8];
+        float pf[CT][8], sum[CT];
 #pragma unroll
         for (int ct = 0; ct < CT; ++ct) {
-          float x[8];
+          if constexpr (cut) {
 #pragma unroll
-          for (int i = 0; i < 8; ++i) {
-            x[i] = s[i >> 2][ct][i & 3];
-            if constexpr (cut) x[i] = n0 + (i >> 2) * 16 + quad * 4 + (i & 3) < see[ct] ? x[i] : kNegInf;
+            for (int i = 0; i < 8; ++i)
+              s[i >> 2][ct][i & 3] = n0 + (i >> 2) * 16 + quad * 4 + (i & 3) < see[ct] ? s[i >> 2][ct][i & 3] : kNegInf;
           }
-          // Probabilities by the reference that there is; only where some of a lane's come to more than kMostSum are the logits' maxima
-          // taken, the reference moved and the probabilities computed again (at first always).
-          auto probabilities = [&]() __attribute__((always_inline)) {
-            float sum = 0.0f;
+          sum[ct] = probabilities(s, ct, pf[ct]);
+        }
+        keep_reference(s, pf, sum);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-              pf[ct][i] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[i], c, -m_run[ct]));
-              sum += pf[ct][i];
-            }
-            return sum;
-          };
-          float sum = probabilities();
-          if (__builtin_expect(__builtin_amdgcn_ballot_w64(!(sum <= kMostSum)) != 0, 0)) {
-            float top = max3f(x[0], x[1], x[2]);
-            top = max3f(top, x[3], x[4]);
-            top = max3f(top, x[5], x[6]);
-            top = quads_max(__builtin_fmaxf(top, x[7])) * c;
-            const float m = __builtin_fmaxf(m_run[ct], top), f = __builtin_amdgcn_exp2f(m_run[ct] - m);
-            m_run[ct] = m;
-            l_run[ct] *= f;
-#pragma unroll
-            for (int d = 0; d < DT; ++d) o[d][ct] *= f;
-            sum = probabilities();
-          }
-          l_run[ct] += sum;
+        for (int ct = 0; ct < CT; ++ct)
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
-            const u32x2 x2 = E::split(pf[ct][2 * i], pf[ct][2 * i + 1]);
-            hi[ct][i] = x2[0];
-            lo[ct][i] = x2[1];
+            hi[ct][i] = E::first(pf[ct][2 * i], pf[ct][2 * i + 1]);
+            lo[ct][i] = E::rest(pf[ct][2 * i], pf[ct][2 * i + 1], hi[ct][i]);
           }
-        }
         // O^T += V^T P^T: 16 features by the keys that the lane's probabilities belong to
-        const u32x4* vst = st + NL * 64;
-        const int vr = quad * 4 + (col >> 2);
-        const uint32_t at = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) const void*)(vst + vr * CPR + (((col >> 1) & 1) ^ swizzle<D>(vr))) + (col & 1) * 8;
+        const uint32_t at = place_v(st + NL * 64);
         bool bad = false;
 #pragma unroll
         for (int d0 = 0; d0 < DT; d0 += 4) {
@@ -340,9 +364,7 @@ struct Part {
       fetch(0, 0);
       if (W == 1 && n_stages > 1) fetch(1, 1);
       __builtin_amdgcn_s_waitcnt(W == 1 ? MINE == 16 ? 0x4F70 : 0x0F70 | MINE : 0x0F70);
-      auto stages = [&](int t0, int t1, auto cut) __attribute__((always_inline)) {
-        for (int t = t0; t < t1; ++t) {
-          const int stage = t & 1;
+      auto turn = [&](int t) __attribute__((always_inline)) {
           if constexpr (W == 1) {  // stage t has landed; the loads of stage t + 1 may be under way
             __builtin_amdgcn_s_waitcnt(MINE == 16 ? 0x4F70 : 0x0F70 | MINE);
             if (t + 1 == n_stages) __builtin_amdgcn_s_waitcnt(0x0F70);
@@ -350,10 +372,15 @@ struct Part {
           } else {
             __builtin_amdgcn_s_waitcnt(0x0F70);
             asm volatile("" ::: "memory");
-            __builtin_amdgcn_s_barrier();  // everyone's part has, and everyone has read stage t - 1, whose place takes stage t + 1
+            __builtin_amdgcn_s_barrier();  // everyone's part has, and everyone has read the stage whose place takes stage t + 1
             asm volatile("" ::: "memory");
-            if (t + 1 < n_stages) fetch(t + 1, stage ^ 1);
+            if (t + 1 < n_stages) fetch(t + 1, (t + 1) % STAGES);
           }
+      };
+      auto stages = [&](int t0, int t1, auto cut) __attribute__((always_inline)) {
+        for (int t = t0; t < t1; ++t) {
+          const int stage = t % STAGES;
+          turn(t);
 #pragma unroll 1
           for (int sub = 0; sub < SUB; ++sub) {
             const int n0 = begin + t * KEYS + sub * kTile;
@@ -366,7 +393,89 @@ struct Part {
       // whole stages that all of the block's queries see, and those behind them (a loop each: where one loop has both kinds of tiles, the
       // compiler moves the outputs from register to register in every tile)
       const int whole = least < end ? least : end, full = whole > begin ? (whole - begin) / KEYS : 0;
-      stages(0, full, std::integral_constant<bool, false>{});
+      if constexpr (PIPE) {
+        // A step has the products of one tile's keys between the exponentials of the tile before, then that one's products with V, the first of
+        // them between the roundings of its probabilities: one after the other, matrix and vector instructions of a SIMD's waves take turns.
+        auto step = [&](const u32x4* st, const u32x4* vst, const f32x4 (&s)[2][CT], f32x4 (&next)[2][CT], auto more) __attribute__((always_inline)) {
+          float pf[CT][8], sum[CT];
+          u32x4 f[2][KK];
+          if constexpr (decltype(more)::value) {
+            read_k(st, f);
+            __builtin_amdgcn_sched_barrier(0);
+            logits(f, next);
+          }
+#pragma unroll
+          for (int ct = 0; ct < CT; ++ct) sum[ct] = probabilities(s, ct, pf[ct]);
+          if constexpr (decltype(more)::value) {
+#pragma unroll
+            for (int i = 0; i < 2 * CT * KK; ++i) {
+              __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+              __builtin_amdgcn_sched_group_barrier(0x002, 24 / (2 * KK), 0);
+            }
+            __builtin_amdgcn_sched_barrier(0);
+          }
+          keep_reference(s, pf, sum);
+          u32x4 hi[CT], lo[CT];
+#pragma unroll
+          for (int ct = 0; ct < CT; ++ct)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) hi[ct][i] = E::first(pf[ct][2 * i], pf[ct][2 * i + 1]);
+          const uint32_t at = place_v(vst);
+#pragma unroll
+          for (int d0 = 0; d0 < DT; d0 += 4) {
+            u32x4 v[4];
+            read_transposed<16 * D * 2>(at, d0, v);
+            if (d0 == 0) __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+#pragma unroll
+              for (int ct = 0; ct < CT; ++ct) o[d0 + i][ct] = E::mfma(v[i], hi[ct], o[d0 + i][ct]);
+            if (d0 == 0) {
+#pragma unroll
+              for (int ct = 0; ct < CT; ++ct)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) lo[ct][i] = E::rest(pf[ct][2 * i], pf[ct][2 * i + 1], hi[ct][i]);
+#pragma unroll
+              for (int i = 0; i < 4 * CT; ++i) {
+                __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+                __builtin_amdgcn_sched_group_barrier(0x002, 5, 0);
+              }
+              __builtin_amdgcn_sched_barrier(0);
+            }
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+#pragma unroll
+              for (int ct = 0; ct < CT; ++ct) o[d0 + i][ct] = E::mfma(v[i], lo[ct], o[d0 + i][ct]);
+          }
+        };
+        if (full > 0) {
+          static_assert(SUB == 2, "two tiles by name");
+          constexpr int TILE = kTile * CPR;
+          f32x4 sa[2][CT], sb[2][CT];
+          turn(0);
+          {
+            u32x4 f[2][KK];
+            read_k(lds, f);
+            logits(f, sa);
+          }
+          step(lds + TILE, lds + NL * 64, sa, sb, std::integral_constant<bool, true>{});
+          asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // all of this stage has been read but for the last values
+          const u32x4* v_last = lds + NL * 64 + TILE;
+#pragma unroll 1
+          for (int t = 1; t < full; ++t) {
+            turn(t);
+            const u32x4* st = lds + t % 3 * STAGE;
+            step(st, v_last, sb, sa, std::integral_constant<bool, true>{});
+            step(st + TILE, st + NL * 64, sa, sb, std::integral_constant<bool, true>{});
+            v_last = st + NL * 64 + TILE;
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+          }
+          step(nullptr, v_last, sb, sa, std::integral_constant<bool, false>{});
+          asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        }
+      } else {
+        stages(0, full, std::integral_constant<bool, false>{});
+      }
       stages(full, n_stages, std::integral_constant<bool, true>{});
     }
     const size_t at = (size_t)(ks.first_split + split) * p.queries;
