@@ -52,6 +52,8 @@ struct Elem {
   }
 };
 
+__device__ __forceinline__ f32x4 mfma_half(u32x4 a, u32x4 b, f32x4 c) { return mfma_f16_16x16x32(as_f16x8(a), as_f16x8(b), c); }
+
 // Tokens of a row of `most`: what the device array says, kept inside the row.
 __device__ __forceinline__ int row_len(const int32_t* lens, int64_t row, int64_t most) {
   if (lens == nullptr) return (int)most;
@@ -126,7 +128,7 @@ struct Part {
   static constexpr int CPR = D / 8, KK = D / 32, DT = D / 16;  // 16-byte pieces per key; products' steps; output tiles
   static constexpr int NL = KEYS * CPR / 64;                   // a stage's loads of K, by a wave
   static constexpr bool PIPE = W == 8;  // products a tile ahead of their exponentials
-  static constexpr int STAGES = PIPE ? 3 : 2, STAGE = 2 * NL * 64;
+  static constexpr int STAGES = PIPE ? 4 : 2, STAGE = 2 * NL * 64;
   static constexpr int MINE = 2 * NL / W;                      // loads of a wave per stage
   static_assert(MINE * W == 2 * NL, "the waves share a stage's loads");
 
@@ -394,16 +396,22 @@ struct Part {
       // compiler moves the outputs from register to register in every tile)
       const int whole = least < end ? least : end, full = whole > begin ? (whole - begin) / KEYS : 0;
       if constexpr (PIPE) {
-        // A step has the products of one tile's keys between the exponentials of the tile before, then that one's products with V, the first of
-        // them between the roundings of its probabilities: one after the other, matrix and vector instructions of a SIMD's waves take turns.
+        // A step has the products of one tile's keys between the exponentials of the tile before, then that one's products with V: one after the
+        // other, matrix and vector instructions of a SIMD's waves take turns.
         auto step = [&](const u32x4* st, const u32x4* vst, const f32x4 (&s)[2][CT], f32x4 (&next)[2][CT], auto more) __attribute__((always_inline)) {
           float pf[CT][8], sum[CT];
-          u32x4 f[2][KK];
-          if constexpr (decltype(more)::value) {
-            read_k(st, f);
-            __builtin_amdgcn_sched_barrier(0);
-            logits(f, next);
+          u32x4 f[2][KK], v[DT];
+          if constexpr (decltype(more)::value) read_k(st, f);
+          const uint32_t at = place_v(vst);
+#pragma unroll
+          for (int d0 = 0; d0 < DT; d0 += 4) {
+            u32x4 x[4];
+            read_transposed<16 * D * 2>(at, d0, x);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) v[d0 + i] = x[i];
           }
+          __builtin_amdgcn_sched_barrier(0);
+          if constexpr (decltype(more)::value) logits(f, next);
 #pragma unroll
           for (int ct = 0; ct < CT; ++ct) sum[ct] = probabilities(s, ct, pf[ct]);
           if constexpr (decltype(more)::value) {
@@ -415,68 +423,123 @@ struct Part {
             __builtin_amdgcn_sched_barrier(0);
           }
           keep_reference(s, pf, sum);
-          u32x4 hi[CT], lo[CT];
+          u32x4 hi[CT];
 #pragma unroll
           for (int ct = 0; ct < CT; ++ct)
 #pragma unroll
-            for (int i = 0; i < 4; ++i) hi[ct][i] = E::first(pf[ct][2 * i], pf[ct][2 * i + 1]);
-          const uint32_t at = place_v(vst);
+            for (int i = 0; i < 4; ++i) hi[ct][i] = Elem<true>::first(pf[ct][2 * i], pf[ct][2 * i + 1]);
 #pragma unroll
-          for (int d0 = 0; d0 < DT; d0 += 4) {
-            u32x4 v[4];
-            read_transposed<16 * D * 2>(at, d0, v);
-            if (d0 == 0) __builtin_amdgcn_sched_barrier(0);
+          for (int d = 0; d < DT; ++d)
 #pragma unroll
-            for (int i = 0; i < 4; ++i)
+            for (int ct = 0; ct < CT; ++ct) o[d][ct] = mfma_half(v[d], hi[ct], o[d][ct]);
+          if constexpr (F16) {
 #pragma unroll
-              for (int ct = 0; ct < CT; ++ct) o[d0 + i][ct] = E::mfma(v[i], hi[ct], o[d0 + i][ct]);
-            if (d0 == 0) {
+            for (int ct = 0; ct < CT; ++ct)
 #pragma unroll
-              for (int ct = 0; ct < CT; ++ct)
+              for (int i = 0; i < 4; ++i) hi[ct][i] = E::rest(pf[ct][2 * i], pf[ct][2 * i + 1], hi[ct][i]);
 #pragma unroll
-                for (int i = 0; i < 4; ++i) lo[ct][i] = E::rest(pf[ct][2 * i], pf[ct][2 * i + 1], hi[ct][i]);
+            for (int d = 0; d < DT; ++d)
 #pragma unroll
-              for (int i = 0; i < 4 * CT; ++i) {
-                __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
-                __builtin_amdgcn_sched_group_barrier(0x002, 5, 0);
-              }
-              __builtin_amdgcn_sched_barrier(0);
-            }
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-#pragma unroll
-              for (int ct = 0; ct < CT; ++ct) o[d0 + i][ct] = E::mfma(v[i], lo[ct], o[d0 + i][ct]);
+              for (int ct = 0; ct < CT; ++ct) o[d][ct] = mfma_half(v[d], hi[ct], o[d][ct]);
           }
         };
+        // V from bf16 to half, in which a probability has three more bits (rounded to bf16 it would need a second product for what that leaves: a
+        // third of all products): every wave its own pieces of a stage, once they have landed, while the stage in front is worked on.  Half
+        // holds a bf16 value exactly from 2^-14 up to 65 504, and below that to 2^-25.  Nothing of a stage with larger ones is used: it
+        // is fetched once more, and from there on all goes the way of the cut stages.  (A word for each of four stages in a row: a wave
+        // that is ahead may have seen the next one's values before another asks for this one's.)
+        uint32_t* beyond = reinterpret_cast<uint32_t*>(lds + STAGES * STAGE);
+        struct Pieces {
+          u32x4 x[NL / W];
+        };
+        auto take = [&](int t, Pieces& y) __attribute__((always_inline)) {
+          if constexpr (!F16) {
+            const u32x4* mine = lds + t % STAGES * STAGE + NL * 64 + wave * 64 + lane;
+#pragma unroll
+            for (int i = 0; i < NL / W; ++i) y.x[i] = mine[i * W * 64];
+          }
+        };
+        auto give = [&](int t, Pieces& y) __attribute__((always_inline)) {
+          if constexpr (!F16) {
+            u32x4* mine = lds + t % STAGES * STAGE + NL * 64 + wave * 64 + lane;
+            bool large = false;
+#pragma unroll
+            for (int i = 0; i < NL / W; ++i) {
+#pragma unroll
+              for (int j = 0; j < 4; ++j) {
+                const uint32_t x = y.x[i][j];
+                large = large || (x & 0x7fffu) >= 0x4780u || (x >> 16 & 0x7fffu) >= 0x4780u;  // 65 536 and above
+                y.x[i][j] = Elem<true>::first(__uint_as_float(x << 16), __uint_as_float(x & 0xffff0000u));
+              }
+              mine[i * W * 64] = y.x[i];
+            }
+            if (__builtin_amdgcn_ballot_w64(large) && lane == 0) beyond[t % 4] = 1u;
+          }
+        };
+        // behind the barrier: whether stage t is all within half
+        auto turn_half = [&](int t) __attribute__((always_inline)) {
+          asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+          __builtin_amdgcn_s_barrier();  // everyone has read stage t - 2 and converted stage t
+          asm volatile("" ::: "memory");
+          const uint32_t odd = F16 ? 0u : *(volatile uint32_t*)(beyond + t % 4);
+          if (t + 2 < n_stages) fetch(t + 2, (t + 2) % STAGES);
+          return odd;
+        };
+        // this wave's part of stage t + 1 has landed; its loads of stage t + 2 may be under way
+        auto next_landed = [&](int t) __attribute__((always_inline)) {
+          __builtin_amdgcn_s_waitcnt(0x0F70 | MINE);
+          if (t + 2 >= n_stages) __builtin_amdgcn_s_waitcnt(0x0F70);
+          asm volatile("" ::: "memory");
+        };
+        int done = 0;
         if (full > 0) {
           static_assert(SUB == 2, "two tiles by name");
           constexpr int TILE = kTile * CPR;
           f32x4 sa[2][CT], sb[2][CT];
-          turn(0);
+          Pieces y;
+          if (n_stages > 1) fetch(1, 1);
+          next_landed(n_stages > 1 ? -1 : 0);
+          take(0, y);
+          give(0, y);
+          uint32_t odd = turn_half(0);
           {
             u32x4 f[2][KK];
             read_k(lds, f);
             logits(f, sa);
           }
-          step(lds + TILE, lds + NL * 64, sa, sb, std::integral_constant<bool, true>{});
-          asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // all of this stage has been read but for the last values
-          const u32x4* v_last = lds + NL * 64 + TILE;
+          if (__builtin_amdgcn_readfirstlane(odd) == 0u) {
+            next_landed(0);
+            if (full > 1) take(1, y);
+            step(lds + TILE, lds + NL * 64, sa, sb, std::integral_constant<bool, true>{});
+            if (full > 1) give(1, y);
+            const u32x4* v_last = lds + NL * 64 + TILE;
+            done = 1;
+            bool pending = true;
 #pragma unroll 1
-          for (int t = 1; t < full; ++t) {
-            turn(t);
-            const u32x4* st = lds + t % 3 * STAGE;
-            step(st, v_last, sb, sa, std::integral_constant<bool, true>{});
-            step(st + TILE, st + NL * 64, sa, sb, std::integral_constant<bool, true>{});
-            v_last = st + NL * 64 + TILE;
+            for (; done < full; ++done) {
+              odd = turn_half(done);
+              const u32x4* st = lds + done % STAGES * STAGE;
+              step(st, v_last, sb, sa, std::integral_constant<bool, true>{});
+              if (__builtin_amdgcn_readfirstlane(odd) != 0u) {
+                pending = false;
+                break;
+              }
+              next_landed(done);
+              if (done + 1 < full) take(done + 1, y);
+              step(st + TILE, st + NL * 64, sa, sb, std::integral_constant<bool, true>{});
+              if (done + 1 < full) give(done + 1, y);
+              v_last = st + NL * 64 + TILE;
+            }
+            if (pending) step(nullptr, v_last, sb, sa, std::integral_constant<bool, false>{});
             asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
           }
-          step(nullptr, v_last, sb, sa, std::integral_constant<bool, false>{});
-          asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+          if (done < full) fetch(done, done % STAGES);
         }
+        stages(done, n_stages, std::integral_constant<bool, true>{});
       } else {
         stages(0, full, std::integral_constant<bool, false>{});
+        stages(full, n_stages, std::integral_constant<bool, true>{});
       }
-      stages(full, n_stages, std::integral_constant<bool, true>{});
     }
     const size_t at = (size_t)(ks.first_split + split) * p.queries;
     if constexpr (V == 1) {
@@ -560,7 +623,9 @@ __global__ __launch_bounds__(64 * V, CT == 1 ? 2 : 1) void attend_wave_kernel(At
 // Many: W waves of 32 queries share the keys.
 template <int D, bool F16, int W>
 __global__ __launch_bounds__(64 * W, W == 2 ? 1 : 2) void attend_block_kernel(AttendArgs a, Plan p, bool shared) {
-  __shared__ u32x4 lds[Part<D, F16, 2, W, 1>::STAGES * Part<D, F16, 2, W, 1>::STAGE];
+  __shared__ u32x4 lds[Part<D, F16, 2, W, 1>::STAGES * Part<D, F16, 2, W, 1>::STAGE + 1];  // (and four words)
+  if (threadIdx.x == 0) lds[Part<D, F16, 2, W, 1>::STAGES * Part<D, F16, 2, W, 1>::STAGE] = u32x4{0, 0, 0, 0};
+  __syncthreads();
   const Keys& ks = shared ? p.shared : p.own;
   int64_t row;
   int split, tile;

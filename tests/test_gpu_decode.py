@@ -4,7 +4,7 @@ weights, the same for a batch on a shared context, eviction by that account, and
 Tolerances.  u = 2^-24.  A logit is a sum of D products of 16-bit values, which fp32 holds exactly; counting two roundings a term, its exponent to
 base 2 is off by at most E = (2 D + 8) u c sum|q||k| with c = log2(e) / sqrt(D).  Softmax numerators and their sum are each off by ln 2 E + 2^-22 relative
 (exp2 included), sums of n terms by another (n / 16 + 64) u (partial sums of at least 16 lanes), a probability split into two 16-bit values by
-2^-16, in fp16 by at least 2^-25 of the largest one.  out is off by that, relative to sum p|v|, and by its own rounding, half a step; weight by the
+2^-16, in fp16 by at least 2^-25 of the largest one; with more than 128 queries a row and bf16 values, one rounded to fp16 by half its step, 2^-12.  out is off by that, relative to sum p|v|, and by its own rounding, half a step; weight by the
 same relative to what is added, the number of its terms times u, and its own rounding."""
 import math
 
@@ -51,7 +51,8 @@ def _check(got, got_w, got_ws, q, k, v, lens, w0, ks=None, vs=None, slens=None, 
             if keys.shape[0] == 0:
                 continue
             E = (2 * D + 8) * U * c * float((q[b, h].reshape(G * T, D).double().abs() @ keys.T).max())
-            rel[b, h] = 2 * (math.log(2) * E + 2.0 ** -22) + ((n + m) / 16 + 64) * U + 2.0 ** -16
+            queries = G * T * (B if m else 1)     # of the row, or of the shared tokens
+            rel[b, h] = 2 * (math.log(2) * E + 2.0 ** -22) + ((n + m) / 16 + 64) * U + (2.0 ** -12 if q.dtype == BF and queries > 128 else 2.0 ** -16)
             most_v[b, h] = float(vals.max()) * (n + m) * 2.0 ** -25
     g = got.double().cpu()
     assert bool(torch.isfinite(g).all()), "non-finite output"
@@ -458,3 +459,28 @@ def test_prune_then_share(ctx):
         assert torch.equal(positions.cpu(), torch.gather(p1, 1, source))
         assert torch.equal(shared.cpu(), torch.gather(s0[0], 1, source.unsqueeze(-1).expand(H, K, D)))
     pk.proxykv_destroy(c)
+
+
+@pytest.mark.parametrize("far", [0, 70, 200, 511, 900])
+def test_attend_many_queries_with_values_beyond_half(ctx, far):
+    """Blocks of many queries multiply bf16 values as half: values up to 65 280 and tiny ones as they are, and from the first key with one of
+    65 536 or more (up to 2^100, or not finite) on, another way; outputs that do not meet it are as near as any."""
+    G, T, N, D = 8, 40, 1001, 128
+    q, k, v = _randn((2, G, T, D), 5, BF), _randn((2, N, D), 6, BF), _randn((2, N, D), 7, BF)
+    v[0, far, ::2], v[1, far, 1::3] = 65280.0, 2.0 ** -30
+    v[1, :, 5] *= 2.0 ** -12
+    lens = torch.tensor([N, N - 1], dtype=torch.int32)
+    w0 = torch.zeros(2, N)
+    for big in (None, 65536.0, 2.0 ** 100):
+        if big is not None:
+            v[0, far, 7], v[1, far, 0] = big, -big
+        w = w0.cuda()
+        out = pk.proxykv_attend(ctx, q.cuda(), k.cuda(), v.cuda(), lens=lens.cuda(), weight=w)
+        torch.cuda.synchronize()
+        _check(out[None], w[None], None, q[None], k[None], v[None], lens[None], w0[None])
+    v[0, far, 7] = float("inf")
+    out = pk.proxykv_attend(ctx, q.cuda(), k.cuda(), v.cuda(), lens=lens.cuda())
+    torch.cuda.synchronize()
+    assert not bool(torch.isfinite(out[0, :, :, 7]).any())
+    keep = [i for i in range(D) if i != 7]
+    assert bool(torch.isfinite(out[0][..., keep]).all()) and bool(torch.isfinite(out[1]).all())
