@@ -247,10 +247,12 @@ int proxykv_compact_pooled(proxykv_ctx* ctx, void* k, void* v, const int32_t* fl
  * weight[r, n] += the sum of the probabilities that token n gets from the row's group * T queries: over a decode, how much of the
  * attention every cached token has had, by which proxykv_evict selects.  The caller clears it for new tokens.
  * Products of q and k run on MFMA with fp32 accumulation, softmax in fp32; for the product with v a probability is split into
- * two 16-bit values.  Results do not depend on what else runs: no sum is taken in an order that varies.
- * D in {64, 128} (PROXYKV_EUNSUPPORTED otherwise), T <= N, rows * group * T < 2^23; weight and lens may lie on any 4-byte boundary.
- * While the stream captures, the call allocates nothing and returns PROXYKV_ESTATE if the context has not served one as large
- * (in each of rows, group * T and N) before: make the largest call once before capturing. */
+ * two 16-bit values, or, where a row has more than 128 queries in bf16, rounded to fp16, relative to about the row's largest.  Results do
+ * not depend on what else runs: no sum is taken in an order that varies.
+ * D in {64, 128} (PROXYKV_EUNSUPPORTED otherwise), T <= N, rows * group * T < 2^22, rows * N < 2^31; weight and lens may lie on any 4-byte
+ * boundary.  out and weight overlap nothing else.
+ * While the stream captures, the call allocates nothing, and returns PROXYKV_ESTATE if it takes more workspace than the context has: one call
+ * before that with the same group * T, no fewer rows, no smaller N, and a weight if this one has it, makes room. */
 int proxykv_attend(proxykv_ctx* ctx, const void* q, const void* k, const void* v, const int32_t* lens,
                    int32_t dtype, int64_t rows, int64_t N, int64_t group, int64_t T, int64_t D, void* out,
                    float* weight, void* stream);
@@ -262,7 +264,8 @@ int proxykv_attend(proxykv_ctx* ctx, const void* q, const void* k, const void* v
  * last of its own; N = 0 (then k, v and lens are not used): there are no own tokens, and the queries see the shared ones.
  *   weight_shared [heads, P] fp32: += what the shared tokens get from all sequences; weight [batch, heads, N] as in proxykv_attend; each
  *   may be NULL.
- * Types, limits and everything else as proxykv_attend, with rows = batch * heads. */
+ * Types, limits (heads * P < 2^31 too), captured calls (no smaller batch, heads, N and P before) and everything else as proxykv_attend, with rows
+ * = batch * heads; the shared tokens' rows have batch * group * T queries. */
 int proxykv_attend_shared(proxykv_ctx* ctx, const void* q, const void* k_shared, const void* v_shared,
                           const int32_t* shared_lens, const void* k, const void* v, const int32_t* lens,
                           int32_t dtype, int64_t batch, int64_t heads, int64_t P, int64_t N, int64_t group,
@@ -278,8 +281,8 @@ int proxykv_attend_shared(proxykv_ctx* ctx, const void* q, const void* k_shared,
  * tokens move).  lens[r] becomes b; what lies behind is left as it was.  Rows of no more than b tokens are not touched.
  *   budgets [rows] int32 (DEVICE): a budget for every row, such as proxykv_topk_pooled's counts, and `budget` is not used; values outside
  *   [recent, N] count as the nearest of the two.  NULL: `budget` for all, 1 <= budget <= N, recent <= budget.
- * 0 <= recent <= N; D*2 bytes a multiple of 16 and at most 512; rows < 2^21.  The workspace (4 bytes * rows * N) and captured calls are as
- * with proxykv_attend. */
+ * 0 <= recent <= N; D*2 bytes a multiple of 16 and at most 512; rows < 2^21.  Captured calls are as with proxykv_attend (no fewer rows and no smaller
+ * N before; the workspace is about 4 bytes * rows * N). */
 int proxykv_evict(proxykv_ctx* ctx, void* k, void* v, float* weight, int32_t* positions, int32_t* lens,
                   const int32_t* budgets, int64_t rows, int64_t N, int64_t budget, int64_t recent, int64_t D,
                   void* stream);

@@ -44,7 +44,7 @@ int validate_config(const proxykv_config* c) {
   return PROXYKV_OK;
 }
 
-constexpr int64_t kAttendQueryUnit = 256;  // work-items of a launch per query: a launch counts them in 32 bits
+constexpr int64_t kAttendQueryUnit = 512;  // bytes of a query's outputs: below 2^31 for all, which also keeps every launch below 2^32 work-items
 
 int validate_lengths(int64_t N, int64_t N_q, int64_t chunk) {
   if (N <= 0 || N_q <= 0 || chunk <= 0) return PROXYKV_EINVAL;
@@ -452,11 +452,12 @@ int attend_impl(proxykv_ctx* ctx, const pkv::AttendArgs& a, int32_t dtype, hipSt
   PKV_HIP(ctx, pkv::launch_attend(a, ctx->attend_ws.ptr, stream));
   return PROXYKV_OK;
 }
-// factors >= 1 whose product stays below 2^31
+
+// whether all are positive and their product is below 2^31
 bool product_fits(std::initializer_list<int64_t> factors) {
   int64_t n = 1;
   for (int64_t f : factors) {
-    if (f <= 0 || f >= (1ll << 31) / n) return false;
+    if (f <= 0 || f > ((1ll << 31) - 1) / n) return false;
     n *= f;
   }
   return true;
@@ -835,7 +836,7 @@ int proxykv_mask(proxykv_ctx* ctx, const int32_t* idx, int64_t rows, int64_t N, 
 int proxykv_attend(proxykv_ctx* ctx, const void* q, const void* k, const void* v, const int32_t* lens, int32_t dtype, int64_t rows, int64_t N,
                    int64_t group, int64_t T, int64_t D, void* out, float* weight, void* stream) {
   if (!ctx || !q || !k || !v || !out) return PROXYKV_EINVAL;
-  if (N <= 0 || N >= (1ll << 31) - 4096 || T > N || D <= 0 || !product_fits({rows, group, T, kAttendQueryUnit})) return PROXYKV_EINVAL;
+  if (N >= (1ll << 31) - 4096 || T > N || D <= 0 || !product_fits({rows, group, T, kAttendQueryUnit}) || !product_fits({rows, N})) return PROXYKV_EINVAL;
   const pkv::AttendArgs a = {q, k, v, nullptr, nullptr, lens, nullptr, out, weight, nullptr, rows, 1, N, 0, group, T, (int)std::min<int64_t>(D, 1 << 20),
                              dtype == PROXYKV_FP16};
   return attend_impl(ctx, a, dtype, (hipStream_t)stream);
@@ -846,7 +847,7 @@ int proxykv_attend_shared(proxykv_ctx* ctx, const void* q, const void* k_shared,
                           int64_t D, void* out, float* weight_shared, float* weight, void* stream) {
   if (!ctx || !q || !k_shared || !v_shared || !out || N < 0 || (N > 0 && (!k || !v))) return PROXYKV_EINVAL;
   if (N >= (1ll << 31) - 4096 || (N > 0 && T > N) || P <= 0 || P >= (1ll << 31) - 4096 || D <= 0 ||
-      !product_fits({batch, heads, group, T, kAttendQueryUnit}))
+      !product_fits({batch, heads, group, T, kAttendQueryUnit}) || !product_fits({heads, P}) || (N > 0 && !product_fits({batch, heads, N})))
     return PROXYKV_EINVAL;
   const pkv::AttendArgs a = {q, k, v, k_shared, v_shared, lens, shared_lens, out, weight, weight_shared, batch, heads, N, P, group, T,
                              (int)std::min<int64_t>(D, 1 << 20), dtype == PROXYKV_FP16};

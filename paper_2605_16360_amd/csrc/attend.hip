@@ -7,9 +7,6 @@
 // computed once more.  No sum's order depends on timing.
 #include "common.hpp"
 #include "kernels.hpp"
-#ifndef PKV_BIG
-#define PKV_BIG 384
-#endif
 
 namespace pkv {
 namespace {
@@ -933,11 +930,13 @@ __global__ __launch_bounds__(256) void attend_add_kernel(float* __restrict__ wei
 }
 
 // Parts of the queries in attend_account_kernel: where a row's keys are few blocks, the last turn on the compute units is mostly empty.
+// (No more blocks than 16 turns have: behind those an empty one is little.  It also bounds the sums that the parts leave.)
+constexpr int64_t kPartBlocks = 4096;
 int account_parts(const Keys& k) {
   const int64_t blocks = k.rows * ((k.n + 255) / 256), steps = (k.m + 63) / 64;
   int best = 1;
   double least = 1e30;
-  for (int p = 1; p <= 8 && p <= steps; ++p) {
+  for (int p = 1; p <= 8 && p <= steps && (p == 1 || blocks * p <= kPartBlocks); ++p) {
     const double turns = (double)((blocks * p + 255) / 256) * (double)((steps + p - 1) / p) + 1.0 * p;
     if (turns < least) {
       least = turns;
@@ -974,7 +973,7 @@ Keys keys_of(int64_t rows, int64_t n, int64_t m, int merge, bool account) {
     if (jobs * splits < 256) splits = (256 + jobs - 1) / jobs;
     least = 256;
   } else {
-    least = jobs * n <= 64 * 256 ? 64 : jobs * n <= 128 * 1024 ? 128 : PKV_BIG;
+    least = jobs * n <= 64 * 256 ? 64 : jobs * n <= 128 * 1024 ? 128 : 384;
     splits = kMostSplits;
   }
   const int64_t most = (n + least - 1) / least;
@@ -989,7 +988,7 @@ Keys keys_of(int64_t rows, int64_t n, int64_t m, int merge, bool account) {
   return k;
 }
 
-size_t plan_of(const AttendArgs& a, Plan* out, uint8_t* scratch) {
+Plan plan_of(const AttendArgs& a, uint8_t* scratch) {
   const int64_t per = a.group * a.T, rows = a.batch * a.heads;
   Plan p = {};
   p.queries = rows * per;
@@ -1014,14 +1013,12 @@ size_t plan_of(const AttendArgs& a, Plan* out, uint8_t* scratch) {
   p.part_sums = take(sums_shared > sums_own ? sums_shared : sums_own);
   if (p.shared.score_stride) p.shared.scores = take((size_t)(p.shared.rows * p.shared.m * p.shared.score_stride));
   if (p.own.score_stride) p.own.scores = take((size_t)(p.own.rows * p.own.m * p.own.score_stride));
-  if (out) *out = p;
-  return at;
+  return p;
 }
 
 template <int D, bool F16>
 hipError_t launch_attend_of(const AttendArgs& a, void* scratch, hipStream_t stream) {
-  Plan p;
-  plan_of(a, &p, (uint8_t*)scratch);
+  const Plan p = plan_of(a, (uint8_t*)scratch);
   hipError_t e = hipSuccess;
   auto many = [&](const Keys& k, bool shared) {
     if (e != hipSuccess || k.waves <= 1) return;
@@ -1082,7 +1079,28 @@ hipError_t launch_attend_of(const AttendArgs& a, void* scratch, hipStream_t stre
 
 }  // namespace
 
-size_t attend_scratch_bytes(const AttendArgs& a) { return plan_of(a, nullptr, nullptr); }
+// Not what this call's plan takes (fewer rows are split more often, so that would shrink and grow), but what none of no more rows, sequences and
+// tokens takes: so one call of the largest size makes room for all.
+size_t attend_scratch_bytes(const AttendArgs& a) {
+  const int64_t per = a.group * a.T, rows = a.batch * a.heads, queries = rows * per;
+  int64_t outputs = 0, scores = 0, sums = 0;
+  auto shares = [&](int64_t rows, int64_t n, int64_t m, bool account) {  // bounds of keys_of's choices, each growing in rows, n and m
+    if (n == 0) return;
+    if (m <= kKeptQueries) {
+      const int64_t s = (n + 383) / 384;
+      outputs += rows * m * (s < kMostSplits ? s : kMostSplits) + kKeptQueries * (1024 + rows);
+      scores += account ? rows * m * ((n + kTile - 1) / kTile * kTile) + 64 : 0;
+    } else {
+      const int64_t tile = m <= 64 ? 64 : m <= 128 ? 128 : 256;
+      outputs += rows * ((m + tile - 1) / tile * tile) + 2048 * 32;
+      sums = account ? kPartBlocks * 256 : sums;
+    }
+  };
+  shares(rows, a.N, per, a.weight != nullptr);
+  shares(a.heads, a.P, a.batch * per, a.weight_shared != nullptr);
+  if (a.batch * per > kKeptQueries) shares(a.heads, a.P, kKeptQueries, a.weight_shared != nullptr);  // a smaller batch
+  return (size_t)(outputs * (a.D + 2) + scores + sums + queries * 2) * 4 + 6 * 256;
+}
 
 hipError_t launch_attend(const AttendArgs& a, void* scratch, hipStream_t stream) {
   if (a.D == 64) return a.f16 ? launch_attend_of<64, true>(a, scratch, stream) : launch_attend_of<64, false>(a, scratch, stream);

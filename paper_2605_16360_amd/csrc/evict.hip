@@ -306,10 +306,6 @@ hipError_t launch_evict(void* k, void* v, float* weight, int32_t* positions, int
     evict_select_kernel<decltype(steps)::value><<<(unsigned)rows, kSelThreads, 0, stream>>>(weight, positions, lens, budgets, N, (int)budget, (int)recent,
                                                                                           (int32_t*)scratch, words);
   };
-#ifdef PKV_STREAM
-  if (1) select(std::integral_constant<int, 0>{});
-  else
-#endif
   if (most <= 2 * kSelThreads) select(std::integral_constant<int, 2>{});
   else if (most <= 5 * kSelThreads) select(std::integral_constant<int, 5>{});
   else if (most <= 10 * kSelThreads) select(std::integral_constant<int, 10>{});
