@@ -947,9 +947,13 @@ int account_parts(const Keys& k) {
 }
 
 constexpr int kMerge = 4;
+#ifndef MKEYS
+#define MKEYS 512
+#endif
+constexpr int64_t kMergedKeys = MKEYS;
 constexpr int64_t kMostSplits = 512;
 
-Keys keys_of(int64_t rows, int64_t n, int64_t m, int merge, bool account) {
+Keys keys_of(int64_t rows, int64_t n, int64_t m, int merge, int64_t more, bool account) {
   Keys k = {};
   k.rows = rows;
   k.n = n;
@@ -969,8 +973,7 @@ Keys keys_of(int64_t rows, int64_t n, int64_t m, int merge, bool account) {
     splits = (2048 / k.waves + jobs - 1) / jobs;
     least = 256;
   } else if (k.merge > 1) {
-    splits = (n + 511) / 512;
-    if (jobs * splits < 256) splits = (256 + jobs - 1) / jobs;
+    splits = (n + kMergedKeys - 1) / kMergedKeys * more;
     least = 256;
   } else {
     least = jobs * n <= 64 * 256 ? 64 : jobs * n <= 128 * 1024 ? 128 : 384;
@@ -995,8 +998,10 @@ Plan plan_of(const AttendArgs& a, uint8_t* scratch) {
   const int64_t m_shared = a.P > 0 ? a.batch * per : 0, m_own = a.N > 0 ? per : 0;
   // waves are joined in LDS where they leave outputs of more than 16 queries: those would be a quarter of what is read
   const int merge = (m_shared > 16 && m_shared <= 32) || (m_own > 16 && m_own <= 32) ? kMerge : 1;
-  p.shared = keys_of(a.heads, a.P, a.batch * per, merge, a.weight_shared != nullptr);
-  p.own = keys_of(rows, a.N, per, merge, a.weight != nullptr);
+  const int64_t blocks = (m_shared <= 32 ? a.heads * ((a.P + kMergedKeys - 1) / kMergedKeys) : 0) + (m_own <= 32 ? rows * ((a.N + kMergedKeys - 1) / kMergedKeys) : 0);
+  const int64_t more = blocks > 0 && blocks < 256 ? 256 / blocks : 1;
+  p.shared = keys_of(a.heads, a.P, m_shared, merge, more, a.weight_shared != nullptr);
+  p.own = keys_of(rows, a.N, m_own, merge, more, a.weight != nullptr);
   p.own.first_split = p.shared.splits;
   p.splits = p.shared.splits + p.own.splits;
   size_t at = 0;
