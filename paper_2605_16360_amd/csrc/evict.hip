@@ -11,7 +11,10 @@ namespace {
 
 constexpr int kSelThreads = 1024, kSelWaves = kSelThreads / 64;
 constexpr int kBins = 2048, kCopies = 8;  // of a digit's histogram: accounts share their high digits, and lanes that meet in a word take turns
-constexpr int kPlanHead = 4;              // words: moves, candidates, keep, recent tokens to move up (0: nothing to do)
+constexpr int kFew = 256;                 // keys that are ranked by comparing all with all
+// Words: moves, candidates, keep, recent tokens to move up (0: nothing to do); then, in order, the places that change: the slots given up, and
+// behind those, as many, the places of the tokens that take them.
+constexpr int kPlanHead = 4;
 
 // Larger key <=> heavier.  NaN maps to 0 (below every number), -0.0 onto +0.0.
 __device__ __forceinline__ uint32_t weight_key(float f) {
@@ -20,22 +23,40 @@ __device__ __forceinline__ uint32_t weight_key(float f) {
   return f == f ? k : 0u;
 }
 
-// One workgroup per row: the keep-th heaviest candidate by a radix select of 11, 11 and 10 bits, the lists of moves in order, then the moves
-// of the account and the positions themselves.  A wave has consecutive candidates, 64 at a time, so that ranks need one exchange
+// One workgroup per row: the keep-th heaviest candidate by a radix select of 11, 11 and 10 bits, which ends where few keys are left in a bin, the list of
+// places that change, then the moves of the account and the positions themselves.  A wave has consecutive candidates, 64 at a time, so that ranks need one exchange
 // between waves.  STEPS > 0: a lane keeps its candidates' keys, STEPS of them, in registers; 0: they are read again for each use.
 template <int STEPS>
 __global__ __launch_bounds__(kSelThreads) void evict_select_kernel(float* __restrict__ weight, int32_t* __restrict__ positions,
                                                                    int32_t* __restrict__ lens, const int32_t* __restrict__ budgets, int64_t N,
                                                                    int budget, int recent, int32_t* __restrict__ plans, int64_t plan_words) {
   __shared__ u32x4 hist4[kBins * kCopies / 4];
-  __shared__ int s_wave[2][kSelWaves];
-  __shared__ uint32_t s_prefix, s_left, s_equal;
-  uint32_t* hist = reinterpret_cast<uint32_t*>(hist4);
+  __shared__ int s_wave[kSelWaves];
+  __shared__ u32x4 few4[kFew / 4];
+  __shared__ uint32_t few_rank[kFew], s_few, s_prefix, s_left, s_equal;
+  uint32_t *hist = reinterpret_cast<uint32_t*>(hist4), *few = reinterpret_cast<uint32_t*>(few4);
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int64_t r = blockIdx.x;
   int32_t* plan = plans + r * plan_words;
-  const int cap = (int)((plan_words - kPlanHead) / 2);
-  int32_t *from = plan + kPlanHead, *to = from + cap;
+  int32_t* list = plan + kPlanHead;
+  float* w = weight + r * N;
+  uint32_t keys[STEPS > 0 ? STEPS : 1];
+  auto ask = [&](int end) __attribute__((always_inline)) {  // (no branch around a load; what lies behind the last candidate counts nowhere)
+#pragma unroll
+    for (int j = 0; j < STEPS; ++j) {
+      const int i = wave * (STEPS * 64) + lane + j * 64;
+      keys[j] = __float_as_uint(w[i < end ? i : end - 1]);
+    }
+  };
+  constexpr bool kAtOnce = STEPS > 0 && STEPS <= 5;  // before the row's length is known: few steps are one wait anyway
+  if constexpr (kAtOnce) ask((int)N);
+  auto clear = [&]() __attribute__((always_inline)) {
+#pragma unroll
+    for (int i = 0; i < kBins * kCopies / 4 / kSelThreads; ++i) hist4[i * kSelThreads + tid] = u32x4{0, 0, 0, 0};
+  };
+  clear();
+  if (tid < kFew) few_rank[tid] = 0;
+  if (tid == 0) s_few = 0;
   int n = lens[r], b = budget;
   n = n < 0 ? 0 : n < N ? n : (int)N;
   if (budgets != nullptr) {
@@ -46,15 +67,12 @@ __global__ __launch_bounds__(kSelThreads) void evict_select_kernel(float* __rest
     if (tid < kPlanHead) plan[tid] = 0;
     return;
   }
-  float* w = weight + r * N;
   const int cand = n - recent, keep = b - recent;
   int moves = 0;
   if (keep > 0) {
     const int steps = STEPS > 0 ? STEPS : (cand + kSelThreads - 1) / kSelThreads, first = wave * steps * 64 + lane;
-    uint32_t keys[STEPS > 0 ? STEPS : 1];
-    if constexpr (STEPS > 0) {  // (no branch around a load; what lies behind the last candidate counts nowhere)
-#pragma unroll
-      for (int j = 0; j < STEPS; ++j) keys[j] = __float_as_uint(w[first + j * 64 < cand ? first + j * 64 : cand - 1]);
+    if constexpr (STEPS > 0) {
+      if constexpr (!kAtOnce) ask(cand);
 #pragma unroll
       for (int j = 0; j < STEPS; ++j) keys[j] = weight_key(__uint_as_float(keys[j]));
     }
@@ -79,11 +97,12 @@ __global__ __launch_bounds__(kSelThreads) void evict_select_kernel(float* __rest
         again(f);
       }
     };
-    uint32_t prefix = 0, left = (uint32_t)keep;
+    uint32_t prefix = 0, left = (uint32_t)keep, equal = kFew + 1;  // of the key's bits known so far, how many keys have them
+    int known = 32;                                                // and how many are not
     static_for<3>([&](auto digit) __attribute__((always_inline)) {
       constexpr int shift = decltype(digit)::value == 0 ? 21 : decltype(digit)::value == 1 ? 10 : 0, bits = decltype(digit)::value == 2 ? 10 : 11;
-#pragma unroll
-      for (int i = 0; i < kBins * kCopies / 4 / kSelThreads; ++i) hist4[i * kSelThreads + tid] = u32x4{0, 0, 0, 0};
+      if (equal <= kFew) return;
+      if constexpr (shift != 21) clear();
       __syncthreads();
       each([&](int i, uint32_t k) __attribute__((always_inline)) {
         if (i < cand && (shift == 21 || (k >> (shift + bits < 32 ? shift + bits : 31)) == (prefix >> (shift + bits < 32 ? shift + bits : 31))))
@@ -102,9 +121,9 @@ __global__ __launch_bounds__(kSelThreads) void evict_select_kernel(float* __rest
         const uint32_t o = __shfl_up(upto, off, 64);
         upto += lane >= off ? o : 0u;
       }
-      if (lane == 63) s_wave[0][wave] = (int)upto;
+      if (lane == 63) s_wave[wave] = (int)upto;
       __syncthreads();
-      for (int x = 0; x < kSelWaves; ++x) upto += x < wave ? (uint32_t)s_wave[0][x] : 0u;
+      for (int x = 0; x < kSelWaves; ++x) upto += x < wave ? (uint32_t)s_wave[x] : 0u;
       uint32_t above = upto - h[0] - h[1];
 #pragma unroll
       for (int e = 0; e < 2; ++e) {
@@ -118,64 +137,81 @@ __global__ __launch_bounds__(kSelThreads) void evict_select_kernel(float* __rest
       __syncthreads();
       prefix = s_prefix;
       left = s_left;
+      equal = s_equal;
+      known = shift;
     });
-    // kept: above the key, or equal to it and among the first `left` of those
-    const uint64_t below = (1ull << lane) - 1;
-    // Lists in order, from what each wave has of them.  walk(f): f(place, given up among the first `keep` places, kept behind them) for this lane's
-    // places in order.
-    auto lists = [&](auto walk) __attribute__((always_inline)) {
-      int holes = 0, fillers = 0;
-      walk([&](int, bool hole, bool filler) __attribute__((always_inline)) {
-        holes += hole;
-        fillers += filler;
+    if (known > 0) {  // the few keys that agree so far: thread t compares the (t % 256)-th with a quarter of them
+      each([&](int i, uint32_t k) __attribute__((always_inline)) {
+        if (i < cand && (k ^ prefix) >> known == 0) few[atomicAdd(&s_few, 1u) % kFew] = k;  // (no more than `equal`)
       });
-      for (int off = 32; off; off >>= 1) {
-        holes += __shfl_xor(holes, off, 64);
-        fillers += __shfl_xor(fillers, off, 64);
-      }
-      if (lane == 0) {
-        s_wave[0][wave] = holes;
-        s_wave[1][wave] = fillers;
+      __syncthreads();
+      const uint32_t x = (uint32_t)tid % kFew, mine = few[x], c = equal;
+      if (x < c) {
+        uint32_t rank = 0;  // greater ones, and equal ones 2^16 each
+        for (uint32_t i = (uint32_t)tid / kFew * 4; i < c; i += kSelThreads / kFew * 4) {
+          const u32x4 y = few4[i / 4];
+#pragma unroll
+          for (uint32_t e = 0; e < 4; ++e) rank += i + e < c ? y[e] > mine ? 1u : y[e] == mine ? 1u << 16 : 0u : 0u;
+        }
+        atomicAdd(&few_rank[x], rank);
       }
       __syncthreads();
-      holes = fillers = 0;
-      for (int x = 0; x < kSelWaves; ++x) {
-        holes += x < wave ? s_wave[0][x] : 0;
-        fillers += x < wave ? s_wave[1][x] : 0;
-        moves += s_wave[1][x];
+      if ((uint32_t)tid < c) {
+        const uint32_t greater = few_rank[tid] & 0xffffu, same = few_rank[tid] >> 16;
+        if (greater < left && greater + same >= left) {  // (of equal keys, all write the same)
+          s_prefix = mine;
+          s_left = left - greater;
+          s_equal = same;
+        }
       }
-      walk([&](int i, bool hole, bool filler) __attribute__((always_inline)) {
-        const uint64_t h = __builtin_amdgcn_ballot_w64(hole), f = __builtin_amdgcn_ballot_w64(filler);
-        if (hole) to[holes + __popcll(h & below)] = i;
-        if (filler) from[fillers + __popcll(f & below)] = i;
-        holes += __popcll(h);
-        fillers += __popcll(f);
+      __syncthreads();
+      prefix = s_prefix;
+      left = s_left;
+      equal = s_equal;
+    }
+    // kept: above the key, or equal to it and among the first `left` of those.  A place changes that is kept behind the first `keep` ones, or
+    // given up among them; walk(f): f(place, kept) for this lane's places in order
+    auto places = [&](auto walk) __attribute__((always_inline)) {
+      int count = 0;
+      walk([&](int i, bool kept) __attribute__((always_inline)) { count += __popcll(__builtin_amdgcn_ballot_w64(kept != (i < keep) && i < cand)); });
+      if (lane == 0) s_wave[wave] = count;
+      __syncthreads();
+      int before = 0;
+      for (int x = 0; x < kSelWaves; ++x) {
+        before += x < wave ? s_wave[x] : 0;
+        moves += s_wave[x];
+      }
+      moves /= 2;
+      walk([&](int i, bool kept) __attribute__((always_inline)) {
+        const bool changes = kept != (i < keep) && i < cand;
+        const uint64_t all = __builtin_amdgcn_ballot_w64(changes);
+        if (changes) list[before + (int)__builtin_amdgcn_mbcnt_hi((uint32_t)(all >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)all, 0))] = i;
+        before += __popcll(all);
       });
     };
-    if (s_equal == left) {  // all of those that equal the key
-      lists([&](auto f) __attribute__((always_inline)) {
-        each([&](int i, uint32_t k) __attribute__((always_inline)) { f(i, i < keep && k < prefix, i >= keep && i < cand && k >= prefix); });
+    if (equal == left) {  // all of those that equal the key
+      places([&](auto f) __attribute__((always_inline)) {
+        each([&](int i, uint32_t k) __attribute__((always_inline)) { f(i, k >= prefix); });
       });
     } else {  // some: by their ranks (masks of a lane's many places take more code than the row's second reading takes time)
       auto stream = [&](auto f) __attribute__((always_inline)) {
         if constexpr (STEPS > 10) again(f);
         else each(f);
       };
-      int equal = 0;
-      stream([&](int i, uint32_t k) __attribute__((always_inline)) { equal += i < cand && k == prefix; });
-      for (int off = 32; off; off >>= 1) equal += __shfl_xor(equal, off, 64);
-      if (lane == 0) s_wave[1][wave] = equal;
+      int count = 0;
+      stream([&](int i, uint32_t k) __attribute__((always_inline)) { count += __popcll(__builtin_amdgcn_ballot_w64(i < cand && k == prefix)); });
+      if (lane == 0) s_wave[wave] = count;
       __syncthreads();
-      int before = 0;
-      for (int x = 0; x < kSelWaves; ++x) before += x < wave ? s_wave[1][x] : 0;
+      int rank0 = 0;
+      for (int x = 0; x < kSelWaves; ++x) rank0 += x < wave ? s_wave[x] : 0;
       __syncthreads();
-      lists([&](auto f) __attribute__((always_inline)) {
-        int rank0 = before;
+      places([&](auto f) __attribute__((always_inline)) {
+        int rank = rank0;
         stream([&](int i, uint32_t k) __attribute__((always_inline)) {
           const uint64_t eq = __builtin_amdgcn_ballot_w64(i < cand && k == prefix);
-          const bool kept = i < cand && (k > prefix || (k == prefix && rank0 + __popcll(eq & below) < (int)left));
-          rank0 += __popcll(eq);
-          f(i, i < keep && !kept, i >= keep && kept);
+          const int mine = rank + (int)__builtin_amdgcn_mbcnt_hi((uint32_t)(eq >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)eq, 0));
+          rank += __popcll(eq);
+          f(i, k > prefix || (k == prefix && mine < (int)left));
         });
       });
     }
@@ -188,10 +224,25 @@ __global__ __launch_bounds__(kSelThreads) void evict_select_kernel(float* __rest
     plan[3] = recent;
   }
   int32_t* pos = positions == nullptr ? nullptr : positions + r * N;
-  for (int j = tid; j < moves; j += kSelThreads) {
-    const int x = from[j], y = to[j];
-    w[y] = w[x];
-    if (pos != nullptr) pos[y] = pos[x];
+  for (int j0 = tid; j0 < moves; j0 += 4 * kSelThreads) {  // (sources lie behind the first `keep` places, targets among them)
+    int y[4], z[4];
+    float x[4];
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      const int j = j0 + u * kSelThreads < moves ? j0 + u * kSelThreads : j0;  // (again the first: the same value once more)
+      y[u] = list[j];
+      z[u] = list[moves + j];
+    }
+#pragma unroll
+    for (int u = 0; u < 4; ++u) x[u] = w[z[u]];
+    if (pos != nullptr) {
+#pragma unroll
+      for (int u = 0; u < 4; ++u) z[u] = pos[z[u]];
+#pragma unroll
+      for (int u = 0; u < 4; ++u) pos[y[u]] = z[u];
+    }
+#pragma unroll
+    for (int u = 0; u < 4; ++u) w[y[u]] = x[u];
   }
   __syncthreads();
   // a recent token never moves back, so what a step stores is behind nothing that a later one reads
@@ -226,7 +277,7 @@ __global__ __launch_bounds__(256) void evict_move_kernel(u32x4* __restrict__ k, 
   const int tid = threadIdx.x, step = 256 * kPer / cps;  // tokens at a time
   const int32_t* plan = plans + r * plan_words;
   const int moves = plan[0], cand = plan[1], keep = plan[2], recent = plan[3], b = keep + recent;
-  const int32_t *from = plan + kPlanHead, *to = from + (plan_words - kPlanHead) / 2;
+  const int32_t *to = plan + kPlanHead, *from = to + plan[0];
   int bound = 0;  // moves from in front of the budget's end: those come first
   for (int lo = 0, hi = moves;;) {
     if (lo >= hi) {
