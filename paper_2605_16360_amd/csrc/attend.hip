@@ -17,6 +17,7 @@ constexpr float kLow = -1.0e30f;        // a reference below every logit that co
 constexpr int kTile = 32;               // keys per step of a wave
 constexpr float kMostSum = 4096.0f;     // of a lane's eight probabilities relative to its query's reference: within fp16, and nothing below is lost
 constexpr int kXcds = 8;
+constexpr int kMerge = 4;               // waves that are joined in LDS
 constexpr int64_t kKeptQueries = 32;    // up to this many queries per key, logits are kept for the account
 
 template <bool F16>
@@ -24,6 +25,9 @@ struct Elem {
   static __device__ __forceinline__ uint16_t narrow(float f) {
     if constexpr (F16) return __builtin_bit_cast(uint16_t, (_Float16)f);
     else return f32_to_bf16_bits(f);
+  }
+  static __device__ __forceinline__ u32x2 narrow4(f32x4 y) {
+    return u32x2{narrow(y[0]) | (uint32_t)narrow(y[1]) << 16, narrow(y[2]) | (uint32_t)narrow(y[3]) << 16};
   }
   static constexpr uint32_t kExp = F16 ? 0x7c00u : 0x7f80u;  // all ones: not finite
   static constexpr uint32_t kOne = F16 ? 0x3c00u : 0x3f80u;
@@ -81,6 +85,7 @@ struct Plan {
   Keys shared, own;
   int64_t queries;
   int splits;      // of both kinds together
+  bool one_launch; // few keys: attend_row_kernel
   float* ml;       // [splits, queries] pairs
   float* o;        // [splits, queries, D]
   float* lse;      // [queries] in the order of q, and behind them in the shared keys' order
@@ -129,7 +134,10 @@ struct Part {
   static constexpr int MINE = 2 * NL / W;                      // loads of a wave per stage
   static_assert(MINE * W == 2 * NL, "the waves share a stage's loads");
 
-  static __device__ __forceinline__ void run(const AttendArgs& a, const Plan& p, const Keys& ks, bool shared, int64_t row, int split, int tile0, u32x4* lds) {
+  // WHOLE: the share is all of a row, whose outputs are written and whose queries' log-sum-exps and sums are left in `fin`.
+  template <bool WHOLE = false>
+  static __device__ __forceinline__ void run(const AttendArgs& a, const Plan& p, const Keys& ks, bool shared, int64_t row, int split, int tile0, u32x4* lds,
+                                             float2* fin = nullptr) {
     const int lane = threadIdx.x & 63, wave = W == 1 ? 0 : __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), col = lane & 15, quad = lane >> 4;
     const int member = V == 1 ? 0 : __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     lds += member * (STAGES * STAGE);
@@ -575,17 +583,26 @@ struct Part {
         const float f = __builtin_amdgcn_exp2f(m_run[ct] - m);
 #pragma unroll
         for (int d = 0; d < DT; ++d) *reinterpret_cast<f32x4*>(all + (member * Q + ct * 16 + col) * LINE + d * 16 + quad * 4) = o[d][ct] * f;
-        if (member == 0 && quad == 0 && m0 + ct * 16 + col < M) reinterpret_cast<float2*>(p.ml)[at + query[ct]] = float2{m, l};
+        if (member == 0 && quad == 0) {
+          if constexpr (WHOLE) fin[ct * 16 + col] = float2{m0 + ct * 16 + col >= M || l == 0.0f ? -kNegInf : m + __builtin_amdgcn_logf(l), l};
+          else if (m0 + ct * 16 + col < M) reinterpret_cast<float2*>(p.ml)[at + query[ct]] = float2{m, l};
+        }
       }
       __syncthreads();
-      if (end0 > begin0) {
+      if (WHOLE || end0 > begin0) {
 #pragma unroll
         for (int i = 0; i < Q * D / 4 / (64 * V); ++i) {
           const int x = i * 64 * V + threadIdx.x, q = x / (D / 4), d = x % (D / 4) * 4;
           f32x4 sum = *reinterpret_cast<const f32x4*>(all + q * LINE + d);
 #pragma unroll
           for (int v = 1; v < V; ++v) sum += *reinterpret_cast<const f32x4*>(all + (v * Q + q) * LINE + d);
-          if (m0 + q < M) *reinterpret_cast<f32x4*>(p.o + (at + query_at(shared, row, m0 + q, per, a.heads)) * D + d) = sum;
+          if constexpr (WHOLE) {
+            const float l = fin[q].y;
+            const u32x2 r = l == 0.0f ? u32x2{0, 0} : Elem<F16>::narrow4(sum / l);
+            if (m0 + q < M) *reinterpret_cast<u32x2*>((uint16_t*)a.out + query_at(shared, row, m0 + q, per, a.heads) * D + d) = r;
+          } else if (m0 + q < M) {
+            *reinterpret_cast<f32x4*>(p.o + (at + query_at(shared, row, m0 + q, per, a.heads)) * D + d) = sum;
+          }
         }
       }
     }
@@ -675,11 +692,7 @@ __device__ __forceinline__ void join_outputs(const AttendArgs& a, const Plan& p,
   }
   if (mine >= p.queries) return;
   const bool none = l == 0.0f;
-  u32x2 r = {0, 0};
-  if (!none) {
-    const f32x4 y = x / l;
-    r = u32x2{Elem<F16>::narrow(y[0]) | (uint32_t)Elem<F16>::narrow(y[1]) << 16, Elem<F16>::narrow(y[2]) | (uint32_t)Elem<F16>::narrow(y[3]) << 16};
-  }
+  const u32x2 r = none ? u32x2{0, 0} : Elem<F16>::narrow4(x / l);
   *reinterpret_cast<u32x2*>((uint16_t*)a.out + query * D + at) = r;
   if (at == 0 && p.lse != nullptr) {
     const float v = none ? -kNegInf : m + __builtin_amdgcn_logf(l);
@@ -751,6 +764,51 @@ __global__ __launch_bounds__(256) void attend_finish_kernel(AttendArgs a, Plan p
   if constexpr (MQ > 0) {
     const bool shared = b < shared_blocks;
     account_kept<D, MQ, KP>(a, p, shared ? p.shared : p.own, shared, shared ? b : b - shared_blocks);
+  }
+}
+
+// A row of few keys and its queries from beginning to end, in one launch: four waves have a quarter of the keys each, and what they leave (one share)
+// is written out by the same block, which has it in its caches.
+template <int D, bool F16>
+__global__ __launch_bounds__(64 * kMerge) void attend_row_kernel(AttendArgs a, Plan p) {
+  using P = Part<D, F16, 1, 1, kMerge>;
+  __shared__ u32x4 lds[kMerge * P::STAGES * P::STAGE];
+  const int64_t row = blockIdx.x;
+  const int M = (int)p.own.m;
+  __shared__ float2 fin[16];
+  P::template run<true>(a, p, p.own, false, row, 0, 0, lds, fin);
+  if (a.weight == nullptr) return;
+  // the account, four keys a thread, from the logits that the block has kept
+  const int T = (int)a.T, len = row_len(a.lens, row, a.N);
+  const float c = kLog2e / __builtin_sqrtf((float)D);
+  float* w = a.weight + row * a.N;
+  const float* scores = p.own.scores + (size_t)row * M * p.own.score_stride;
+  for (int n = threadIdx.x * 4; n < len; n += 64 * kMerge * 4) {
+    f32x4 s[16];
+    float x[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) x[e] = w[n + e < len ? n + e : len - 1];
+    static_for<4>([&](auto quarter) __attribute__((always_inline)) {
+      constexpr int q = decltype(quarter)::value * 4;
+      if (q >= M) return;
+#pragma unroll
+      for (int m = q; m < q + 4; ++m) s[m] = *reinterpret_cast<const f32x4*>(scores + (size_t)(m < M ? m : M - 1) * p.own.score_stride + n);
+    });
+    float sum[4] = {};
+    static_for<4>([&](auto quarter) __attribute__((always_inline)) {
+      constexpr int q = decltype(quarter)::value * 4;
+      if (q >= M) return;
+#pragma unroll
+      for (int m = q; m < q + 4; ++m) {
+        const float ref = fin[m].x;
+        const int see = m < M ? seen(len, T, m % T) : 0;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) sum[e] += n + e < see ? __builtin_amdgcn_exp2f(__builtin_fmaf(s[m][e], c, -ref)) : 0.0f;
+      }
+    });
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      if (n + e < len) w[n + e] = x[e] + sum[e];
   }
 }
 
@@ -946,9 +1004,12 @@ int account_parts(const Keys& k) {
   return best;
 }
 
-constexpr int kMerge = 4;
 constexpr int64_t kMergedKeys = 512;  // of a share (64 rows of up to 4001 keys, 20 queries: 25.2 us, 256 keys 28.8; 8 of 9830, 32 queries, with 64 of 512: 22.9 and 29.8)
 constexpr int64_t kMostSplits = 512;
+// One launch instead of two (which takes the host 3.5 us less of about 17) where a block per row is not much slower on the device: us, one and two
+// launches, 4 query heads: 4 rows of 256 keys 6.7 and 7.9, 4 of up to 512 8.9 and 8.0, 256 of 512 15.2 and 17.1; but 8 of 1024 12.8 and
+// 8.1, and with more rows than compute units (a block has most of one's LDS) 1024 of 128 27.5 and 19.0.
+constexpr int64_t kShortKeys = 512, kShortRows = 256;
 
 Keys keys_of(int64_t rows, int64_t n, int64_t m, int merge, int64_t more, bool account) {
   Keys k = {};
@@ -970,7 +1031,7 @@ Keys keys_of(int64_t rows, int64_t n, int64_t m, int merge, int64_t more, bool a
     splits = (2048 / k.waves + jobs - 1) / jobs;
     least = 256;
   } else if (k.merge > 1) {
-    splits = (n + kMergedKeys - 1) / kMergedKeys * more;
+    splits = more == 0 ? 1 : (n + kMergedKeys - 1) / kMergedKeys * more;
     least = 256;
   } else {
     least = jobs * n <= 64 * 256 ? 64 : jobs * n <= 128 * 1024 ? 128 : 384;
@@ -992,11 +1053,13 @@ Plan plan_of(const AttendArgs& a, uint8_t* scratch) {
   const int64_t per = a.group * a.T, rows = a.batch * a.heads;
   Plan p = {};
   p.queries = rows * per;
+  const bool short_rows = a.P == 0 && per <= 16 && a.N <= kShortKeys && rows <= kShortRows;
   const int64_t m_shared = a.P > 0 ? a.batch * per : 0, m_own = a.N > 0 ? per : 0;
   // waves are joined in LDS where they leave outputs of more than 16 queries: those would be a quarter of what is read
-  const int merge = (m_shared > 16 && m_shared <= 32) || (m_own > 16 && m_own <= 32) ? kMerge : 1;
+  const int merge = short_rows || (m_shared > 16 && m_shared <= 32) || (m_own > 16 && m_own <= 32) ? kMerge : 1;
   const int64_t blocks = (m_shared <= 32 ? a.heads * ((a.P + kMergedKeys - 1) / kMergedKeys) : 0) + (m_own <= 32 ? rows * ((a.N + kMergedKeys - 1) / kMergedKeys) : 0);
-  const int64_t more = blocks > 0 && blocks < 256 ? 256 / blocks : 1;
+  const int64_t more = short_rows ? 0 : blocks > 0 && blocks < 256 ? 256 / blocks : 1;
+  p.one_launch = short_rows;
   p.shared = keys_of(a.heads, a.P, m_shared, merge, more, a.weight_shared != nullptr);
   p.own = keys_of(rows, a.N, m_own, merge, more, a.weight != nullptr);
   p.own.first_split = p.shared.splits;
@@ -1022,6 +1085,10 @@ template <int D, bool F16>
 hipError_t launch_attend_of(const AttendArgs& a, void* scratch, hipStream_t stream) {
   const Plan p = plan_of(a, (uint8_t*)scratch);
   hipError_t e = hipSuccess;
+  if (p.one_launch) {
+    attend_row_kernel<D, F16><<<(unsigned)p.own.rows, 64 * kMerge, 0, stream>>>(a, p);
+    return hipGetLastError();
+  }
   auto many = [&](const Keys& k, bool shared) {
     if (e != hipSuccess || k.waves <= 1) return;
     if (k.waves == 2) attend_block_kernel<D, F16, 2><<<(unsigned)k.blocks, 128, 0, stream>>>(a, p, shared);

@@ -122,6 +122,15 @@ def test_attend_long_rows_and_many(ctx, rows, G, T, N):
     _attend(ctx, rows, G, T, N, 64, HF, lens, seed=N + 50)
 
 
+@pytest.mark.parametrize("rows,G,T,N", [(256, 4, 1, 512), (257, 4, 1, 512), (256, 1, 1, 1), (257, 2, 3, 40), (9, 4, 1, 511), (9, 4, 1, 512), (9, 4, 1, 513), (9, 16, 1, 512),
+                                        (9, 17, 1, 512), (9, 2, 8, 513), (9, 1, 1, 545), (9, 4, 4, 640)])
+def test_attend_few_keys_and_one_more(ctx, rows, G, T, N):
+    """Rows that one workgroup takes from beginning to end, and what is a row, a query or a token more than that; empty rows among them."""
+    lens = [0 if r % 5 == 3 else N - (r * 37) % (N // 2 + 1) for r in range(rows)]
+    _attend(ctx, rows, G, T, N, 128, BF, lens, seed=N + rows)
+    _attend(ctx, rows, G, T, N, 64, HF, lens, seed=N + rows + 9, weight=False)
+
+
 @pytest.mark.parametrize("scale", [0.0, 8.0, 60.0])
 @pytest.mark.parametrize("dtype", [BF, HF])
 def test_attend_flat_and_sharp_logits(ctx, scale, dtype):
