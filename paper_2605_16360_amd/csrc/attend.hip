@@ -714,9 +714,13 @@ __device__ __forceinline__ void account_kept(const AttendArgs& a, const Plan& p,
   if (b % blocks * (256 * KP) >= len) return;
   // (asked for before the joins: score rows have room for a whole quad)
   keys_t s[MQ];
+  static_for<MQ / 4>([&](auto four) __attribute__((always_inline)) {
+    constexpr int q = decltype(four)::value * 4;
+    if (q >= M) return;
 #pragma unroll
-  for (int m = 0; m < MQ; ++m)
-    s[m] = *reinterpret_cast<const keys_t*>(ks.scores + ((size_t)row * M + (m < M ? m : M - 1)) * ks.score_stride + (n < len ? n : 0));
+    for (int m = q; m < q + 4; ++m)
+      s[m] = *reinterpret_cast<const keys_t*>(ks.scores + ((size_t)row * M + (m < M ? m : M - 1)) * ks.score_stride + (n < len ? n : 0));
+  });
   float* w = (shared ? a.weight_shared : a.weight) + row * ks.n;
   float x[KP];
 #pragma unroll
@@ -744,13 +748,19 @@ __device__ __forceinline__ void account_kept(const AttendArgs& a, const Plan& p,
   __syncthreads();
   const float c = kLog2e / __builtin_sqrtf((float)D);
   float sum[KP] = {};
+  int t = 0;  // m % T
+  static_for<MQ / 4>([&](auto four) __attribute__((always_inline)) {
+    constexpr int q = decltype(four)::value * 4;
+    if (q >= M) return;
 #pragma unroll
-  for (int m = 0; m < MQ; ++m) {
-    const float ref = lse[m];
-    const int see = m < M ? shared ? len : seen(len, T, m % T) : 0;
+    for (int m = q; m < q + 4; ++m) {
+      const float ref = lse[m];
+      const int see = m < M ? shared ? len : seen(len, T, t) : 0;
+      t = t + 1 == T ? 0 : t + 1;
 #pragma unroll
-    for (int e = 0; e < KP; ++e) sum[e] += n + e < see ? __builtin_amdgcn_exp2f(__builtin_fmaf(s[m][e], c, -ref)) : 0.0f;
-  }
+      for (int e = 0; e < KP; ++e) sum[e] += n + e < see ? __builtin_amdgcn_exp2f(__builtin_fmaf(s[m][e], c, -ref)) : 0.0f;
+    }
+  });
 #pragma unroll
   for (int e = 0; e < KP; ++e)
     if (n + e < len) w[n + e] = x[e] + sum[e];
@@ -795,13 +805,15 @@ __global__ __launch_bounds__(64 * kMerge) void attend_row_kernel(AttendArgs a, P
       for (int m = q; m < q + 4; ++m) s[m] = *reinterpret_cast<const f32x4*>(scores + (size_t)(m < M ? m : M - 1) * p.own.score_stride + n);
     });
     float sum[4] = {};
+    int t = 0;  // m % T
     static_for<4>([&](auto quarter) __attribute__((always_inline)) {
       constexpr int q = decltype(quarter)::value * 4;
       if (q >= M) return;
 #pragma unroll
       for (int m = q; m < q + 4; ++m) {
         const float ref = fin[m].x;
-        const int see = m < M ? seen(len, T, m % T) : 0;
+        const int see = m < M ? seen(len, T, t) : 0;
+        t = t + 1 == T ? 0 : t + 1;
 #pragma unroll
         for (int e = 0; e < 4; ++e) sum[e] += n + e < see ? __builtin_amdgcn_exp2f(__builtin_fmaf(s[m][e], c, -ref)) : 0.0f;
       }
@@ -1118,8 +1130,9 @@ hipError_t launch_attend_of(const AttendArgs& a, void* scratch, hipStream_t stre
     attend_finish_kernel<D, F16, QB, MQ, KP><<<(unsigned)(query_blocks + shared_blocks + own_blocks), 256, 0, stream>>>(a, p, query_blocks, (int)shared_blocks);
   };
   auto finish_of = [&](auto qb) {
-    auto with = [&](auto mq) {  // four keys a thread where that still gives every compute unit two blocks
-      if (kept_keys >= 512 * 1024) finish(qb, mq, std::integral_constant<int, 4>{});
+    // Four keys a thread where most compute units still get a block (256 064 of them: 22.4 us a call, one a thread 24.5; 111 408: 24.2 and 23.6).
+    auto with = [&](auto mq) {
+      if (kept_keys >= 192 * 1024) finish(qb, mq, std::integral_constant<int, 4>{});
       else finish(qb, mq, std::integral_constant<int, 1>{});
     };
     if (kept == 0) finish(qb, std::integral_constant<int, 0>{}, std::integral_constant<int, 1>{});
