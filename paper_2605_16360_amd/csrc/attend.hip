@@ -1,10 +1,15 @@
 // Attention of new tokens over the compacted cache (what the target does with it after the mask was applied), with an account of the softmax
 // weight that every cached token gets.
 //
-// Three steps.  attend_part_kernel: waves take shares of a row's keys (a row's new tokens are few, its keys many) and leave, for each query, the
-// share's running maximum m, sum l of 2^(c s - m) and unscaled output.  attend_finish_kernel: shares are joined, in order, and where the logits
-// were kept, every key's probabilities are added to the account.  attend_account_kernel: where they were not (many queries), they are
-// computed once more.  No sum's order depends on timing.
+// Three steps.  attend_wave_kernel and, for more than 32 queries per key, attend_block_kernel: waves take shares of a row's keys (a row's new tokens
+// are few, its keys many) and leave, for each query, the share's reference m, its sum l of 2^(c s - m), c = log2(e) / sqrt(D), and its unscaled
+// output, in fp32.  attend_finish_kernel: shares are joined, in order, and where the logits were kept, every key's probabilities are added to the
+// account.  attend_account_kernel: where they were not (many queries), they are computed once more.  Rows of few keys go through
+// attend_row_kernel, which does all of it.  No sum's order depends on timing.
+//
+// A tile is 32 keys.  S^T = K Q^T on 16 x 16 x 32 matrix instructions: a lane has one query (column) and 8 of the keys, so that a softmax needs
+// nothing from other lanes but a sum over four of them at the end, and its probabilities are the second product's operand as they lie (O^T =
+// V^T P^T); V is transposed on its way out of LDS.  K and V go into LDS without registers, two stages ahead.
 #include "common.hpp"
 #include "kernels.hpp"
 
@@ -621,7 +626,10 @@ __device__ __forceinline__ bool share_of(int b, const Keys& ks, int64_t& row, in
   return share < ks.rows * ks.splits;
 }
 
-// Few queries per row: V waves for a share of its keys.  CT: of the kind of keys that has the larger tiles.
+// Few queries per row: V waves for a share of its keys.  CT: of the kind of keys that has the larger tiles.  Bound by reading the cache: 256 rows of up
+// to 8192 keys, 4 queries, 540 MB in 117 us (4.6 TB/s; a large copy reaches 5.2), 8 rows of 10 240 in 10.5.  Waves of their own, five of
+// which fit a compute unit's LDS, rather than blocks: nothing waits for anything but its own loads.  From 17 queries on what a share leaves is a quarter
+// of what it reads, and four waves are joined first (64 rows of up to 4001 keys of 64, 20 queries: 15 us).
 template <int D, bool F16, int CT, int V>
 __global__ __launch_bounds__(64 * V, CT == 1 ? 2 : 1) void attend_wave_kernel(AttendArgs a, Plan p) {
   __shared__ u32x4 lds[V * Part<D, F16, CT, 1, V>::STAGES * Part<D, F16, CT, 1, V>::STAGE];
@@ -634,7 +642,10 @@ __global__ __launch_bounds__(64 * V, CT == 1 ? 2 : 1) void attend_wave_kernel(At
   else Part<D, F16, CT, 1, V>::run(a, p, ks, shared, row, split, tile, lds);
 }
 
-// Many: W waves of 32 queries share the keys.
+// Many: W waves of 32 queries share the keys.  2048 queries on 10 343 keys of 128 for each of 8 heads (W = 8), 8.7e10 flop, take 119 us, 256 on 32 768
+// 51 (0.73 and 0.67 PFLOP/s; a large library product reaches 1.25).  The matrix unit is busy for 37 % of that, and no one thing bounds the rest: without
+// the reads of K out of LDS it would be 17 us less, without those of V 5, without exponentials 8, without the products with V 13.  Half of the waves
+// half a step behind the others and other orders of products and exponentials left the time as it is.
 template <int D, bool F16, int W>
 __global__ __launch_bounds__(64 * W, W == 2 ? 1 : 2) void attend_block_kernel(AttendArgs a, Plan p, bool shared) {
   __shared__ u32x4 lds[Part<D, F16, 2, W, 1>::STAGES * Part<D, F16, 2, W, 1>::STAGE + 1];  // (and four words)
@@ -647,8 +658,8 @@ __global__ __launch_bounds__(64 * W, W == 2 ? 1 : 2) void attend_block_kernel(At
   Part<D, F16, 2, W, 1>::run(a, p, ks, shared, row, split, tile, lds);
 }
 
-// Joins the shares' outputs: D / 4 threads hold a share's row, so that a block takes 4 queries of few shares (QB = 4), or one query's
-// 256 / (D / 4) shares at a time.
+// Joins the shares' outputs: D / 4 threads hold a share's row, so that a block takes 4 queries of few shares (QB = 4), or one query's 256 / (D / 4)
+// shares at a time.  Bound by reading them: 16 384 queries of four shares, 36 MB and 4.5 MB written in 11.9 us.
 template <int D, bool F16, int QB>
 __device__ __forceinline__ void join_outputs(const AttendArgs& a, const Plan& p, int block) {
   constexpr int LPR = D / 4, G = 256 / LPR / QB;  // threads per row; shares at a time
@@ -702,7 +713,8 @@ __device__ __forceinline__ void join_outputs(const AttendArgs& a, const Plan& p,
   }
 }
 
-// The account of 256 * KP keys of a row from logits that were kept, of up to MQ queries.
+// The account of 256 * KP keys of a row from logits that were kept, of up to MQ queries: a chain of loads (lengths; logits, sums and the account; then
+// the store) that takes 3 us where little is to be done, otherwise bound by reading the logits (256 rows of up to 8192, 34 MB, 12 us with the outputs).
 template <int D, int MQ, int KP>
 __device__ __forceinline__ void account_kept(const AttendArgs& a, const Plan& p, const Keys& ks, bool shared, int b) {
   typedef float keys_t __attribute__((ext_vector_type(KP)));
@@ -777,8 +789,8 @@ __global__ __launch_bounds__(256) void attend_finish_kernel(AttendArgs a, Plan p
   }
 }
 
-// A row of few keys and its queries from beginning to end, in one launch: four waves have a quarter of the keys each, and what they leave (one share)
-// is written out by the same block, which has it in its caches.
+// A row of few keys and its queries from beginning to end, in one launch: four waves have a quarter of the keys each and are joined in LDS, and the logits,
+// for the account, come out of the compute unit's own cache.  A chain of waits: 4 rows of up to 512 keys 8.9 us, of 256 6.7.
 template <int D, bool F16>
 __global__ __launch_bounds__(64 * kMerge) void attend_row_kernel(AttendArgs a, Plan p) {
   using P = Part<D, F16, 1, 1, kMerge>;
@@ -828,6 +840,9 @@ __global__ __launch_bounds__(64 * kMerge) void attend_row_kernel(AttendArgs a, P
 // them, or one of `parts` parts of those, 64 at a time, through LDS.  S: a lane has the logits of its key (column) with queries 4 quad + r, so
 // that a key's sum stays in the lane until the end.  The products of 16 queries are spread between the exponentials of the 16 before: one
 // after the other, matrix and vector instructions of a SIMD's waves take turns.  Sums of parts are added up by attend_add_kernel.
+// 2048 queries on 10 343 keys of 128 for 8 heads, 4.3e10 flop and 1.7e8 exponentials, take 61 us, 256 on 32 768 31, with the vector unit busy for 53 % of
+// the time and the matrix unit for 34.  Three blocks per compute unit, 1 to 8 parts, and 32 x 32 products with the exponentials spread from step to step
+// took as long (the last at a clock of 2.03 GHz where this has 2.2).
 template <int D, bool F16>
 __global__ __launch_bounds__(256, 2) void attend_account_kernel(AttendArgs a, Keys ks, bool shared, const float* __restrict__ lse, int parts,
                                                                 float* __restrict__ part_sums) {
