@@ -314,6 +314,24 @@ def test_evict_narrow_range_of_weights(ctx):
     _evict(ctx, 4, 4000, 64, [4000, 4000, 4000, 3999], 3000, 17, seed=5, w=w)
 
 
+@pytest.mark.parametrize("N", [1500, 12000, 45000])
+@pytest.mark.parametrize("same,bits", [(255, 21), (256, 21), (257, 21), (256, 10), (257, 10), (600, 10)])
+def test_evict_keys_that_agree_in_front(ctx, N, same, bits):
+    """The weight that decides is among `same` ones that differ in their last `bits` bits at most, some of them equal, as many as are ranked by comparison
+    and one more; the budget ends at the first, the last, and in between."""
+    g = torch.Generator().manual_seed(same + bits)
+    rows, w = 6, torch.rand(6, N, generator=g) * 0.5
+    w[:, ::2] += 2.0                                        # half above, half below the ones that agree, near 1.0
+    for r in range(rows):
+        at = torch.randperm(N - 5, generator=g)[:same]
+        low = torch.randint(0, 1 << bits, (same,), generator=g, dtype=torch.int32)
+        low[:5] = low[0]
+        w[r, at] = (low + 0x3f800000).view(torch.float32)
+    heavy = [int((w[r, :N - 5] >= 2).sum()) for r in range(rows)]
+    budgets = [5 + heavy[0] + 1, 5 + heavy[1] + same, 5 + heavy[2] + same // 2, 5 + heavy[3] + 3, 5 + heavy[4], 5 + heavy[5] + same + 1]
+    _evict(ctx, rows, N, 8, [N] * rows, None, 5, seed=N + same, budgets=budgets, w=w)
+
+
 def test_evict_beyond_two_to_the_31_elements(ctx):
     rows, N, D = 64, 300001, 128
     k, v = torch.empty(rows, N, D, dtype=BF, device="cuda"), torch.empty(rows, N, D, dtype=BF, device="cuda")
@@ -394,6 +412,47 @@ def test_calls_in_a_graph(ctx):
         graph.replay()
         torch.cuda.synchronize()
         for x, y in zip((out, k, v, w, lens), ref):
+            assert torch.equal(x, y)
+
+
+@pytest.mark.parametrize("B,H,G,T,P,N,D,dtype", [(1, 6, 4, 1, 0, 300, 128, BF), (1, 3, 4, 5, 0, 900, 64, HF), (1, 2, 4, 70, 0, 1100, 128, BF), (1, 2, 3, 16, 0, 777, 64, BF),
+                                                  (3, 2, 4, 1, 800, 40, 128, BF), (40, 2, 4, 1, 900, 33, 128, BF), (5, 2, 4, 1, 700, 64, 64, HF)])
+def test_every_kind_of_launch_in_a_graph(ctx, B, H, G, T, P, N, D, dtype):
+    """One launch and several, kept logits and those that are computed again, in parts and not: three replays on new contents, eager calls of the same context in
+    front of each, equal to those bit for bit."""
+    q, out = (torch.zeros(B, H, G, T, D, dtype=dtype, device="cuda") for _ in range(2))
+    k, v = (torch.zeros(B, H, N, D, dtype=dtype, device="cuda") for _ in range(2))
+    ks, vs = (torch.zeros(H, max(P, 1), D, dtype=dtype, device="cuda") for _ in range(2))
+    w, ws = torch.zeros(B, H, N, device="cuda"), torch.zeros(H, max(P, 1), device="cuda")
+    lens = torch.tensor([[N - (b * H + h) % 7 for h in range(H)] for b in range(B)], dtype=torch.int32, device="cuda")
+
+    def fill(seed):
+        for i, x in enumerate((q, k, v, ks, vs)):
+            x.copy_(_randn(x.shape, seed + i, dtype))
+        w.fill_(0.5)
+        ws.zero_()
+
+    def step():
+        if P:
+            pk.proxykv_attend_shared(ctx, q, ks, vs, k, v, lens=lens, weight_shared=ws, weight=w, out=out)
+        else:
+            pk.proxykv_attend(ctx, q, k, v, lens=lens, weight=w, out=out)
+
+    fill(0)
+    step()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step()
+    for seed in (10, 20, 30):
+        fill(seed)
+        step()
+        torch.cuda.synchronize()
+        ref = [x.clone() for x in (out, w, ws)]
+        fill(seed)
+        graph.replay()
+        torch.cuda.synchronize()
+        for x, y in zip((out, w, ws), ref):
             assert torch.equal(x, y)
 
 
