@@ -406,21 +406,11 @@ struct Part {
       // compiler moves the outputs from register to register in every tile)
       const int whole = least < end ? least : end, full = whole > begin ? (whole - begin) / KEYS : 0;
       if constexpr (PIPE) {
-        // A step has the products of one tile's keys between the exponentials of the tile before, then that one's products with V: one after the
-        // other, matrix and vector instructions of a SIMD's waves take turns.
-        auto step = [&](const u32x4* st, const u32x4* vst, const f32x4 (&s)[2][CT], f32x4 (&next)[2][CT], auto more) __attribute__((always_inline)) {
+        // A step has the products of one tile's keys (f, read a step ahead) between the exponentials of the tile before, then that one's products with
+        // V: one after the other, matrix and vector instructions of a SIMD's waves take turns.  `ahead` reads the next keys in front of the latter.
+        auto step = [&](u32x4 (&f)[2][KK], const u32x4* vst, const f32x4 (&s)[2][CT], f32x4 (&next)[2][CT], auto more, auto ahead)
+            __attribute__((always_inline)) {
           float pf[CT][8], sum[CT];
-          u32x4 f[2][KK], v[DT];
-          if constexpr (decltype(more)::value) read_k(st, f);
-          const uint32_t at = place_v(vst);
-#pragma unroll
-          for (int d0 = 0; d0 < DT; d0 += 4) {
-            u32x4 x[4];
-            read_transposed<16 * D * 2>(at, d0, x);
-#pragma unroll
-            for (int i = 0; i < 4; ++i) v[d0 + i] = x[i];
-          }
-          __builtin_amdgcn_sched_barrier(0);
           if constexpr (decltype(more)::value) logits(f, next);
 #pragma unroll
           for (int ct = 0; ct < CT; ++ct) sum[ct] = probabilities(s, ct, pf[ct]);
@@ -438,19 +428,33 @@ struct Part {
           for (int ct = 0; ct < CT; ++ct)
 #pragma unroll
             for (int i = 0; i < 4; ++i) hi[ct][i] = Elem<true>::first(pf[ct][2 * i], pf[ct][2 * i + 1]);
-#pragma unroll
-          for (int d = 0; d < DT; ++d)
-#pragma unroll
-            for (int ct = 0; ct < CT; ++ct) o[d][ct] = mfma_half(v[d], hi[ct], o[d][ct]);
+          u32x4 lo[CT];
           if constexpr (F16) {
 #pragma unroll
             for (int ct = 0; ct < CT; ++ct)
 #pragma unroll
-              for (int i = 0; i < 4; ++i) hi[ct][i] = E::rest(pf[ct][2 * i], pf[ct][2 * i + 1], hi[ct][i]);
+              for (int i = 0; i < 4; ++i) lo[ct][i] = E::rest(pf[ct][2 * i], pf[ct][2 * i + 1], hi[ct][i]);
+          }
+          __builtin_amdgcn_sched_barrier(0);
+          ahead();
+          __builtin_amdgcn_sched_barrier(0);
+          const uint32_t at = place_v(vst);
 #pragma unroll
-            for (int d = 0; d < DT; ++d)
+          for (int d0 = 0; d0 < DT; d0 += 4) {
+            u32x4 x[4];
+            read_transposed<16 * D * 2>(at, d0, x);
+            __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-              for (int ct = 0; ct < CT; ++ct) o[d][ct] = mfma_half(v[d], hi[ct], o[d][ct]);
+            for (int d = 0; d < 4; ++d)
+#pragma unroll
+              for (int ct = 0; ct < CT; ++ct) o[d0 + d][ct] = mfma_half(x[d], hi[ct], o[d0 + d][ct]);
+            if constexpr (F16) {
+#pragma unroll
+              for (int d = 0; d < 4; ++d)
+#pragma unroll
+                for (int ct = 0; ct < CT; ++ct) o[d0 + d][ct] = mfma_half(x[d], lo[ct], o[d0 + d][ct]);
+            }
+            __builtin_amdgcn_sched_barrier(0);
           }
         };
         // V from bf16 to half, in which a probability has three more bits (rounded to bf16 it would need a second product for what that leaves: a
@@ -506,41 +510,34 @@ struct Part {
           static_assert(SUB == 2, "two tiles by name");
           constexpr int TILE = kTile * CPR;
           f32x4 sa[2][CT], sb[2][CT];
+          u32x4 f[2][KK];
           Pieces y;
           if (n_stages > 1) fetch(1, 1);
           next_landed(n_stages > 1 ? -1 : 0);
           take(0, y);
           give(0, y);
-          uint32_t odd = turn_half(0);
-          {
-            u32x4 f[2][KK];
+          uint32_t odd = __builtin_amdgcn_readfirstlane(turn_half(0));
+          if (odd == 0u) {
             read_k(lds, f);
             logits(f, sa);
-          }
-          if (__builtin_amdgcn_readfirstlane(odd) == 0u) {
-            next_landed(0);
-            if (full > 1) take(1, y);
-            step(lds + TILE, lds + NL * 64, sa, sb, std::integral_constant<bool, true>{});
-            if (full > 1) give(1, y);
-            const u32x4* v_last = lds + NL * 64 + TILE;
-            done = 1;
-            bool pending = true;
+            read_k(lds + TILE, f);
 #pragma unroll 1
-            for (; done < full; ++done) {
-              odd = turn_half(done);
-              const u32x4* st = lds + done % STAGES * STAGE;
-              step(st, v_last, sb, sa, std::integral_constant<bool, true>{});
-              if (__builtin_amdgcn_readfirstlane(odd) != 0u) {
-                pending = false;
-                break;
-              }
+            for (; done + 1 < full; ++done) {  // sa: of the first tile of stage `done`, f: the second one's keys
+              const u32x4 *st = lds + done % STAGES * STAGE, *on = lds + (done + 1) % STAGES * STAGE;
               next_landed(done);
-              if (done + 1 < full) take(done + 1, y);
-              step(st + TILE, st + NL * 64, sa, sb, std::integral_constant<bool, true>{});
-              if (done + 1 < full) give(done + 1, y);
-              v_last = st + NL * 64 + TILE;
+              take(done + 1, y);
+              step(f, st + NL * 64, sa, sb, std::integral_constant<bool, true>{}, [&]() __attribute__((always_inline)) {
+                give(done + 1, y);
+                odd = __builtin_amdgcn_readfirstlane(turn_half(done + 1));
+                read_k(on, f);
+              });
+              if (odd != 0u) break;
+              step(f, st + NL * 64 + TILE, sb, sa, std::integral_constant<bool, true>{}, [&]() __attribute__((always_inline)) { read_k(on + TILE, f); });
             }
-            if (pending) step(nullptr, v_last, sb, sa, std::integral_constant<bool, false>{});
+            const u32x4* st = lds + done % STAGES * STAGE;
+            if (odd == 0u) step(f, st + NL * 64, sa, sb, std::integral_constant<bool, true>{}, []() {});
+            step(f, st + NL * 64 + TILE, sb, sa, std::integral_constant<bool, false>{}, []() {});
+            ++done;
             asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
           }
           if (done < full) fetch(done, done % STAGES);
@@ -645,7 +642,7 @@ __global__ __launch_bounds__(64 * V, CT == 1 ? 2 : 1) void attend_wave_kernel(At
 // Many: W waves of 32 queries share the keys.  2048 queries on 10 343 keys of 128 for each of 8 heads (W = 8), 8.7e10 flop, take 119 us, 256 on 32 768
 // 51 (0.73 and 0.67 PFLOP/s; a large library product reaches 1.25).  The matrix unit is busy for 37 % of that, and no one thing bounds the rest: without
 // the reads of K out of LDS it would be 17 us less, without those of V 5, without exponentials 8, without the products with V 13.  Half of the waves
-// half a step behind the others and other orders of products and exponentials left the time as it is.
+// half a step behind the others were 2 % slower, and orders of products and exponentials or wave priorities made no difference.
 template <int D, bool F16, int W>
 __global__ __launch_bounds__(64 * W, W == 2 ? 1 : 2) void attend_block_kernel(AttendArgs a, Plan p, bool shared) {
   __shared__ u32x4 lds[Part<D, F16, 2, W, 1>::STAGES * Part<D, F16, 2, W, 1>::STAGE + 1];  // (and four words)
