@@ -253,7 +253,8 @@ int proxykv_compact_pooled(proxykv_ctx* ctx, void* k, void* v, const int32_t* fl
  * D in {64, 128} (PROXYKV_EUNSUPPORTED otherwise), T <= N, rows * group * T < 2^22, rows * N < 2^31; weight and lens may lie on any 4-byte
  * boundary.  out and weight overlap nothing else.
  * While the stream captures, the call allocates nothing, and returns PROXYKV_ESTATE if it takes more workspace than the context has: one call
- * before that with the same group * T, no fewer rows, no smaller N, and a weight if this one has it, makes room. */
+ * before that with the same group * T, no fewer rows, no smaller N, and a weight if this one has it, makes room.  Graphs that hold calls of one
+ * context share its workspace: they are replayed one behind the other. */
 int proxykv_attend(proxykv_ctx* ctx, const void* q, const void* k, const void* v, const int32_t* lens,
                    int32_t dtype, int64_t rows, int64_t N, int64_t group, int64_t T, int64_t D, void* out,
                    float* weight, void* stream);

@@ -300,6 +300,13 @@ def test_evict_budgets_of_their_own(ctx):
     _evict(ctx, 8, 800, 128, [800, 800, 800, 700, 700, 64, 65, 800], None, 64, seed=3, budgets=[100, 64, 3, 699, 700, 64, 64, 5000])
 
 
+def test_evict_to_nothing_and_nothing_but_the_recent(ctx):
+    """Budgets of no token, of fewer than none, of one, and of the recent tokens alone."""
+    _evict(ctx, 6, 90, 64, [90, 90, 1, 0, 90, 2], None, 0, seed=8, budgets=[0, -7, 0, 0, 1, 1])
+    _evict(ctx, 3, 90, 64, [90, 41, 40], 40, 40, seed=9)
+    _evict(ctx, 3, 2100, 64, [2100, 1300, 1299], 1300, 1300, seed=10)
+
+
 @pytest.mark.parametrize("rows,N,budget,recent", [(2, 40000, 30000, 500), (1, 170000, 51000, 1024), (300, 600, 580, 128), (3, 36864, 36863, 0), (2, 36865, 20000, 20000)])
 def test_evict_long_rows_and_many(ctx, rows, N, budget, recent):
     _evict(ctx, rows, N, 64, [N - (r % 7) for r in range(rows)], budget, recent, seed=N)
