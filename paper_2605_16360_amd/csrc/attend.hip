@@ -655,8 +655,9 @@ __global__ __launch_bounds__(64 * W, W == 2 ? 1 : 2) void attend_block_kernel(At
   Part<D, F16, 2, W, 1>::run(a, p, ks, shared, row, split, tile, lds);
 }
 
-// Joins the shares' outputs: D / 4 threads hold a share's row, so that a block takes 4 queries of few shares (QB = 4), or one query's 256 / (D / 4)
-// shares at a time.  Bound by reading them: 16 384 queries of four shares, 36 MB and 4.5 MB written in 11.9 us.
+// Joins the shares' outputs: D / 4 threads hold a share's row, so that a block takes 8 queries of up to four shares (QB = 8), 4 of up to eight, or one
+// query's 256 / (D / 4) shares at a time.  Bound by reading them: 16 384 queries of four shares, 36 MB and 4.5 MB written, 9 us (with QB = 4, where half
+// of the reads are another's share once more, 11.5).
 template <int D, bool F16, int QB>
 __device__ __forceinline__ void join_outputs(const AttendArgs& a, const Plan& p, int block) {
   constexpr int LPR = D / 4, G = 256 / LPR / QB;  // threads per row; shares at a time
@@ -1153,7 +1154,8 @@ hipError_t launch_attend_of(const AttendArgs& a, void* scratch, hipStream_t stre
     else if (kept <= 16) with(std::integral_constant<int, 16>{});
     else with(std::integral_constant<int, 32>{});
   };
-  if (p.splits <= 8) finish_of(std::integral_constant<int, 4>{});
+  if (p.splits <= 4) finish_of(std::integral_constant<int, 8>{});
+  else if (p.splits <= 8) finish_of(std::integral_constant<int, 4>{});
   else finish_of(std::integral_constant<int, 1>{});
   e = hipGetLastError();
   auto account = [&](const Keys& k, bool shared, float* weight, const int32_t* lens, const float* lse) {
