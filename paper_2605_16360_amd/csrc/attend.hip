@@ -58,8 +58,6 @@ struct Elem {
   }
 };
 
-__device__ __forceinline__ f32x4 mfma_half(u32x4 a, u32x4 b, f32x4 c) { return mfma_f16_16x16x32(as_f16x8(a), as_f16x8(b), c); }
-
 // Tokens of a row of `most`: what the device array says, kept inside the row.
 __device__ __forceinline__ int row_len(const int32_t* lens, int64_t row, int64_t most) {
   if (lens == nullptr) return (int)most;
@@ -423,18 +421,14 @@ struct Part {
             __builtin_amdgcn_sched_barrier(0);
           }
           keep_reference(s, pf, sum);
-          u32x4 hi[CT];
+          u32x4 hi[CT], lo[CT];
 #pragma unroll
           for (int ct = 0; ct < CT; ++ct)
 #pragma unroll
-            for (int i = 0; i < 4; ++i) hi[ct][i] = Elem<true>::first(pf[ct][2 * i], pf[ct][2 * i + 1]);
-          u32x4 lo[CT];
-          if constexpr (F16) {
-#pragma unroll
-            for (int ct = 0; ct < CT; ++ct)
-#pragma unroll
-              for (int i = 0; i < 4; ++i) lo[ct][i] = E::rest(pf[ct][2 * i], pf[ct][2 * i + 1], hi[ct][i]);
-          }
+            for (int i = 0; i < 4; ++i) {
+              hi[ct][i] = E::first(pf[ct][2 * i], pf[ct][2 * i + 1]);
+              lo[ct][i] = E::rest(pf[ct][2 * i], pf[ct][2 * i + 1], hi[ct][i]);
+            }
           __builtin_amdgcn_sched_barrier(0);
           ahead();
           __builtin_amdgcn_sched_barrier(0);
@@ -447,57 +441,20 @@ struct Part {
 #pragma unroll
             for (int d = 0; d < 4; ++d)
 #pragma unroll
-              for (int ct = 0; ct < CT; ++ct) o[d0 + d][ct] = mfma_half(x[d], hi[ct], o[d0 + d][ct]);
-            if constexpr (F16) {
+              for (int ct = 0; ct < CT; ++ct) o[d0 + d][ct] = E::mfma(x[d], hi[ct], o[d0 + d][ct]);
 #pragma unroll
-              for (int d = 0; d < 4; ++d)
+            for (int d = 0; d < 4; ++d)
 #pragma unroll
-                for (int ct = 0; ct < CT; ++ct) o[d0 + d][ct] = mfma_half(x[d], lo[ct], o[d0 + d][ct]);
-            }
+              for (int ct = 0; ct < CT; ++ct) o[d0 + d][ct] = E::mfma(x[d], lo[ct], o[d0 + d][ct]);
             __builtin_amdgcn_sched_barrier(0);
           }
         };
-        // V from bf16 to half, in which a probability has three more bits (rounded to bf16 it would need a second product for what that leaves: a
-        // third of all products): every wave its own pieces of a stage, once they have landed, while the stage in front is worked on.  Half
-        // holds a bf16 value exactly from 2^-14 up to 65 504, and below that to 2^-25.  Nothing of a stage with larger ones is used: it
-        // is fetched once more, and from there on all goes the way of the cut stages.  (A word for each of four stages in a row: a wave
-        // that is ahead may have seen the next one's values before another asks for this one's.)
-        uint32_t* beyond = reinterpret_cast<uint32_t*>(lds + STAGES * STAGE);
-        struct Pieces {
-          u32x4 x[NL / W];
-        };
-        auto take = [&](int t, Pieces& y) __attribute__((always_inline)) {
-          if constexpr (!F16) {
-            const u32x4* mine = lds + t % STAGES * STAGE + NL * 64 + wave * 64 + lane;
-#pragma unroll
-            for (int i = 0; i < NL / W; ++i) y.x[i] = mine[i * W * 64];
-          }
-        };
-        auto give = [&](int t, Pieces& y) __attribute__((always_inline)) {
-          if constexpr (!F16) {
-            u32x4* mine = lds + t % STAGES * STAGE + NL * 64 + wave * 64 + lane;
-            bool large = false;
-#pragma unroll
-            for (int i = 0; i < NL / W; ++i) {
-#pragma unroll
-              for (int j = 0; j < 4; ++j) {
-                const uint32_t x = y.x[i][j];
-                large = large || (x & 0x7fffu) >= 0x4780u || (x >> 16 & 0x7fffu) >= 0x4780u;  // 65 536 and above
-                y.x[i][j] = Elem<true>::first(__uint_as_float(x << 16), __uint_as_float(x & 0xffff0000u));
-              }
-              mine[i * W * 64] = y.x[i];
-            }
-            if (__builtin_amdgcn_ballot_w64(large) && lane == 0) beyond[t % 4] = 1u;
-          }
-        };
-        // behind the barrier: whether stage t is all within half
-        auto turn_half = [&](int t) __attribute__((always_inline)) {
+        // behind its barrier stage t may be read
+        auto turn_ahead = [&](int t) __attribute__((always_inline)) {
           asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-          __builtin_amdgcn_s_barrier();  // everyone has read stage t - 2 and converted stage t
+          __builtin_amdgcn_s_barrier();  // everyone's part of stage t has landed, and everyone has read stage t - 2, whose place takes stage t + 2
           asm volatile("" ::: "memory");
-          const uint32_t odd = F16 ? 0u : *(volatile uint32_t*)(beyond + t % 4);
           if (t + 2 < n_stages) fetch(t + 2, (t + 2) % STAGES);
-          return odd;
         };
         // this wave's part of stage t + 1 has landed; its loads of stage t + 2 may be under way
         auto next_landed = [&](int t) __attribute__((always_inline)) {
@@ -511,36 +468,27 @@ struct Part {
           constexpr int TILE = kTile * CPR;
           f32x4 sa[2][CT], sb[2][CT];
           u32x4 f[2][KK];
-          Pieces y;
           if (n_stages > 1) fetch(1, 1);
           next_landed(n_stages > 1 ? -1 : 0);
-          take(0, y);
-          give(0, y);
-          uint32_t odd = __builtin_amdgcn_readfirstlane(turn_half(0));
-          if (odd == 0u) {
-            read_k(lds, f);
-            logits(f, sa);
-            read_k(lds + TILE, f);
+          turn_ahead(0);
+          read_k(lds, f);
+          logits(f, sa);
+          read_k(lds + TILE, f);
 #pragma unroll 1
-            for (; done + 1 < full; ++done) {  // sa: of the first tile of stage `done`, f: the second one's keys
-              const u32x4 *st = lds + done % STAGES * STAGE, *on = lds + (done + 1) % STAGES * STAGE;
-              next_landed(done);
-              take(done + 1, y);
-              step(f, st + NL * 64, sa, sb, std::integral_constant<bool, true>{}, [&]() __attribute__((always_inline)) {
-                give(done + 1, y);
-                odd = __builtin_amdgcn_readfirstlane(turn_half(done + 1));
-                read_k(on, f);
-              });
-              if (odd != 0u) break;
-              step(f, st + NL * 64 + TILE, sb, sa, std::integral_constant<bool, true>{}, [&]() __attribute__((always_inline)) { read_k(on + TILE, f); });
-            }
-            const u32x4* st = lds + done % STAGES * STAGE;
-            if (odd == 0u) step(f, st + NL * 64, sa, sb, std::integral_constant<bool, true>{}, []() {});
-            step(f, st + NL * 64 + TILE, sb, sa, std::integral_constant<bool, false>{}, []() {});
-            ++done;
-            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+          for (; done + 1 < full; ++done) {  // sa: of the first tile of stage `done`, f: the second one's keys
+            const u32x4 *st = lds + done % STAGES * STAGE, *on = lds + (done + 1) % STAGES * STAGE;
+            next_landed(done);
+            step(f, st + NL * 64, sa, sb, std::integral_constant<bool, true>{}, [&]() __attribute__((always_inline)) {
+              turn_ahead(done + 1);
+              read_k(on, f);
+            });
+            step(f, st + NL * 64 + TILE, sb, sa, std::integral_constant<bool, true>{}, [&]() __attribute__((always_inline)) { read_k(on + TILE, f); });
           }
-          if (done < full) fetch(done, done % STAGES);
+          const u32x4* st = lds + done % STAGES * STAGE;
+          step(f, st + NL * 64, sa, sb, std::integral_constant<bool, true>{}, []() {});
+          step(f, st + NL * 64 + TILE, sb, sa, std::integral_constant<bool, false>{}, []() {});
+          ++done;
+          asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
         }
         stages(done, n_stages, std::integral_constant<bool, true>{});
       } else {
@@ -645,9 +593,7 @@ __global__ __launch_bounds__(64 * V, CT == 1 ? 2 : 1) void attend_wave_kernel(At
 // half a step behind the others were 2 % slower, and orders of products and exponentials or wave priorities made no difference.
 template <int D, bool F16, int W>
 __global__ __launch_bounds__(64 * W, W == 2 ? 1 : 2) void attend_block_kernel(AttendArgs a, Plan p, bool shared) {
-  __shared__ u32x4 lds[Part<D, F16, 2, W, 1>::STAGES * Part<D, F16, 2, W, 1>::STAGE + 1];  // (and four words)
-  if (threadIdx.x == 0) lds[Part<D, F16, 2, W, 1>::STAGES * Part<D, F16, 2, W, 1>::STAGE] = u32x4{0, 0, 0, 0};
-  __syncthreads();
+  __shared__ u32x4 lds[Part<D, F16, 2, W, 1>::STAGES * Part<D, F16, 2, W, 1>::STAGE];
   const Keys& ks = shared ? p.shared : p.own;
   int64_t row;
   int split, tile;

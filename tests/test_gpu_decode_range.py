@@ -1,0 +1,92 @@
+"""What attention keeps of small and large values, of probabilities far below the largest, of infinities and of extreme logits, on every kind of launch: rows of
+up to 16, 32, 64, 128 and more queries.
+
+Tolerances.  u = 2^-24; E, the error of a logit's exponent to base 2, is at most (2 D + 8) u c sum|q||k| with c = log2(e) / sqrt(D): two roundings a term,
+and the products of 16-bit values are exact in fp32.  Softmax numerators and their sum are each off by ln 2 E + 2^-22 relative (exp2 included), sums of n terms by
+(n / 16 + 64) u (partial sums of at least 16 lanes), a probability that is split into two values of the type by half a step of half a step, 2^-16 in bf16 and
+2^-22 in fp16, all relative to sum p|v|.  Out adds its own rounding, half a step (of fp16 below 2^-14 half of 2^-24)."""
+import math
+
+import pytest
+import torch
+
+import oracle
+from paper_2605_16360_amd import binding as pk
+from paper_2605_16360_amd import synth
+
+pytestmark = pytest.mark.gpu
+U = 2.0 ** -24
+BF, HF = torch.bfloat16, torch.float16
+# (query heads, new tokens): rows of 4, 16, 20, 52, 120, 132 and 520 queries, which every kind of launch is among
+QUERIES = [(4, 1), (4, 4), (4, 5), (4, 13), (8, 15), (4, 33), (8, 65)]
+
+
+@pytest.fixture(scope="module")
+def ctx():
+    c = pk.proxykv_create(pk.config_for_case(synth.CASES["tiny"]))
+    yield c
+    torch.cuda.synchronize()
+    pk.proxykv_destroy(c)
+
+
+def _randn(shape, seed, dtype, scale=1.0):
+    g = torch.Generator().manual_seed(seed)
+    return (torch.randn(*shape, generator=g) * scale).to(dtype)
+
+
+def _bounds(q, k, v, lens):
+    """(out, weight) of the oracle and what each may be off by, without any allowance that is not relative to what is summed."""
+    rows, G, T, D = q.shape
+    out, w, _, spread = oracle.attend(q[None], k[None], v[None], lens[None])
+    n = k.shape[1]
+    mass = (q.double().abs().reshape(rows, G * T, D) @ k.double().abs().transpose(1, 2)).amax((1, 2)).view(rows, 1, 1, 1)
+    rel = 2 * (math.log(2) * (2 * D + 8) * U * 1.4427 / math.sqrt(D) * mass + 2.0 ** -22) + (n / 16 + 64) * U
+    half = torch.finfo(q.dtype).eps / 2
+    split = half ** 2 * 1.01
+    least = 2.0 ** -25 if q.dtype == HF else 0.0
+    tol_out = spread[0] * (rel + split) + half * (1 + 2.0 ** -8) * out[0].abs() + least
+    tol_w = w[0] * (rel[:, 0, 0] + (G * T + 2) * U)
+    return out[0], tol_out, w[0], tol_w
+
+
+def _within(got, ref, tol, name):
+    g = got.double().cpu()
+    assert bool(torch.isfinite(g).all()), f"{name}: not finite"
+    err = (g - ref).abs()
+    assert bool((err <= tol).all()), f"{name}: worst {float((err / tol.clamp_min(1e-300)).max()):.3g} of the bound, max abs err {float(err.max()):.3e}"
+
+
+def _attend(ctx, q, k, v, lens=None, account=True):
+    lens = torch.full((k.shape[0],), k.shape[1], dtype=torch.int32) if lens is None else torch.tensor(lens, dtype=torch.int32)
+    w = torch.zeros(k.shape[:2], device="cuda") if account else None
+    out = pk.proxykv_attend(ctx, q.cuda(), k.cuda(), v.cuda(), lens=lens.cuda(), weight=w)
+    torch.cuda.synchronize()
+    ref, tol, w_ref, w_tol = _bounds(q, k, v, lens)
+    _within(out, ref, tol, "out")
+    if account:
+        _within(w, w_ref, w_tol, "weight")
+
+
+# ---- the bits of values and of probabilities ------------------------------------------------------------------------
+
+@pytest.mark.parametrize("G,T", QUERIES)
+@pytest.mark.parametrize("dtype,scale", [(BF, 1e-8), (BF, 2.0 ** -60), (BF, 2.0 ** 60), (HF, 2.0 ** -12), (HF, 2.0 ** 12)])
+def test_values_of_every_size_are_kept(ctx, G, T, dtype, scale):
+    """Values that are all small or all large, however many queries there are."""
+    for D, N in ((128, 700), (64, 333)):
+        _attend(ctx, _randn((2, G, T, D), T, dtype), _randn((2, N, D), T + 1, dtype), _randn((2, N, D), T + 2, dtype, scale), [N, N - 70])
+
+
+@pytest.mark.parametrize("G,T", QUERIES)
+@pytest.mark.parametrize("dtype", [BF, HF])
+def test_probabilities_are_not_one_16_bit_value(ctx, G, T, dtype):
+    """Two keys of nearly the same logit with opposite values among keys without any: out is the difference of two probabilities, to the bits of both."""
+    D, N = 64, 192
+    q = torch.zeros(2, G, T, D)
+    q[..., 0], q[..., 1] = 2.0, _randn((2, G, T), 3, dtype).float() * 0.01
+    k = torch.zeros(2, N, D)
+    k[:, 5, 0] = k[:, 70, 0] = 4.0
+    k[:, 70, 1] = 4.0
+    v = torch.zeros(2, N, D)
+    v[:, 5], v[:, 70] = 1.0, -1.0
+    _attend(ctx, q.to(dtype), k.to(dtype), v.to(dtype), account=False)
