@@ -247,7 +247,7 @@ int proxykv_compact_pooled(proxykv_ctx* ctx, void* k, void* v, const int32_t* fl
  * weight[r, n] += the sum of the probabilities that token n gets from the row's group * T queries: over a decode, how much of the
  * attention every cached token has had, by which proxykv_evict selects.  The caller clears it for new tokens.
  * Products of q and k run on MFMA with fp32 accumulation, softmax in fp32; for the product with v a probability is the sum of two values of the
- * cache's type (what rounding leaves of it is at most 2^-16 of it in bf16, 2^-22 in fp16), for any number of queries. Results do not depend on what else runs: no sum is taken in an order
+ * cache's type (what rounding leaves of it is at most 2^-16 of it in bf16; in fp16 2^-22, and no less than 2^-36 of the query's largest), for any number of queries. Results do not depend on what else runs: no sum is taken in an order
  * that varies.
  * D in {64, 128} (PROXYKV_EUNSUPPORTED otherwise), T <= N, rows * group * T < 2^22, rows * N < 2^31; weight and lens may lie on any 4-byte
  * boundary.  out and weight overlap nothing else.

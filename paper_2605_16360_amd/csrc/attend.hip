@@ -20,7 +20,6 @@ constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kNegInf = -__builtin_huge_valf();
 constexpr float kLow = -1.0e30f;        // a reference below every logit that counts
 constexpr int kTile = 32;               // keys per step of a wave
-constexpr float kMostSum = 4096.0f;     // of a lane's eight probabilities relative to its query's reference: within fp16, and nothing below is lost
 constexpr int kXcds = 8;
 constexpr int kMerge = 4;               // waves that are joined in LDS
 constexpr int64_t kKeptQueries = 32;    // up to this many queries per key, logits are kept for the account
@@ -36,6 +35,9 @@ struct Elem {
   }
   static constexpr uint32_t kExp = F16 ? 0x7c00u : 0x7f80u;  // all ones: not finite
   static constexpr uint32_t kOne = F16 ? 0x3c00u : 0x3f80u;
+  // Probabilities are relative to their query's reference, which lies kBelow under the largest logit (base 2) whenever it moves; it moves when a
+  // lane's eight come to more than kMostSum.  fp16 has steps of 2^-24 at its low end, so its largest ones begin at 2^11: 2^-36 of that is left.
+  static constexpr float kBelow = F16 ? 11.0f : 0.0f, kMostSum = F16 ? 32768.0f : 4096.0f;
   static __device__ __forceinline__ f32x4 mfma(u32x4 a, u32x4 b, f32x4 c) {
     if constexpr (F16) return mfma_f16_16x16x32(as_f16x8(a), as_f16x8(b), c);
     else return mfma_bf16_16x16x32(as_bf16x8(a), as_bf16x8(b), c);
@@ -224,7 +226,7 @@ struct Part {
 #pragma unroll
             for (int ct = 0; ct < CT; ++ct) s[kt][ct] = E::mfma(f[kt][kk], bq[ct][kk], s[kt][ct]);
       };
-      // Probabilities by the reference that there is; only where some of a lane's come to more than kMostSum are the logits' maxima taken, the
+      // Probabilities by the reference that there is; only where a lane's come to more than kMostSum are the logits' maxima taken, the
       // reference moved and the probabilities computed again (at first always).
       auto probabilities = [&](const f32x4 (&s)[2][CT], int ct, float (&pf)[8]) __attribute__((always_inline)) {
         float sum = 0.0f;
@@ -238,7 +240,7 @@ struct Part {
       auto keep_reference = [&](const f32x4 (&s)[2][CT], float (&pf)[CT][8], float (&sum)[CT]) __attribute__((always_inline)) {
         bool much = false;
 #pragma unroll
-        for (int ct = 0; ct < CT; ++ct) much = much || !(sum[ct] <= kMostSum);
+        for (int ct = 0; ct < CT; ++ct) much = much || !(sum[ct] <= E::kMostSum);
         if (__builtin_expect(__builtin_amdgcn_ballot_w64(much) != 0, 0)) {
 #pragma unroll
           for (int ct = 0; ct < CT; ++ct) {
@@ -246,7 +248,7 @@ struct Part {
             top = max3f(top, s[0][ct][3], s[1][ct][0]);
             top = max3f(top, s[1][ct][1], s[1][ct][2]);
             top = quads_max(__builtin_fmaxf(top, s[1][ct][3])) * c;
-            const float m = __builtin_fmaxf(m_run[ct], top), f = __builtin_amdgcn_exp2f(m_run[ct] - m);
+            const float m = __builtin_fmaxf(m_run[ct], top - E::kBelow), f = __builtin_amdgcn_exp2f(m_run[ct] - m);
             m_run[ct] = m;
             l_run[ct] *= f;
 #pragma unroll

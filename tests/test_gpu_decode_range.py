@@ -4,7 +4,8 @@ up to 16, 32, 64, 128 and more queries.
 Tolerances.  u = 2^-24; E, the error of a logit's exponent to base 2, is at most (2 D + 8) u c sum|q||k| with c = log2(e) / sqrt(D): two roundings a term,
 and the products of 16-bit values are exact in fp32.  Softmax numerators and their sum are each off by ln 2 E + 2^-22 relative (exp2 included), sums of n terms by
 (n / 16 + 64) u (partial sums of at least 16 lanes), a probability that is split into two values of the type by half a step of half a step, 2^-16 in bf16 and
-2^-22 in fp16, all relative to sum p|v|.  Out adds its own rounding, half a step (of fp16 below 2^-14 half of 2^-24)."""
+2^-22 in fp16, all relative to sum p|v|; in fp16, where the largest
+probability of a share is at least 2^11 and the smallest step 2^-24, by at least 2^-36 of the largest one, times the largest value.  Out adds its own rounding, half a step (of fp16 below 2^-14 half of 2^-24)."""
 import math
 
 import pytest
@@ -43,9 +44,9 @@ def _bounds(q, k, v, lens):
     rel = 2 * (math.log(2) * (2 * D + 8) * U * 1.4427 / math.sqrt(D) * mass + 2.0 ** -22) + (n / 16 + 64) * U
     half = torch.finfo(q.dtype).eps / 2
     split = half ** 2 * 1.01
-    least = 2.0 ** -25 if q.dtype == HF else 0.0
+    least = 2.0 ** -25 + n * 2.0 ** -36 * float(v.abs().max()) if q.dtype == HF else 0.0
     tol_out = spread[0] * (rel + split) + half * (1 + 2.0 ** -8) * out[0].abs() + least
-    tol_w = w[0] * (rel[:, 0, 0] + (G * T + 2) * U)
+    tol_w = w[0] * (rel[:, 0, 0] + (G * T + 2) * U) + G * T * 2.0 ** -126  # (fp32 has no full precision below 2^-126: the smallest of each query's terms may be lost)
     return out[0], tol_out, w[0], tol_w
 
 
@@ -90,3 +91,28 @@ def test_probabilities_are_not_one_16_bit_value(ctx, G, T, dtype):
     v = torch.zeros(2, N, D)
     v[:, 5], v[:, 70] = 1.0, -1.0
     _attend(ctx, q.to(dtype), k.to(dtype), v.to(dtype), account=False)
+
+
+@pytest.mark.parametrize("G,T", QUERIES)
+@pytest.mark.parametrize("dtype", [BF, HF])
+@pytest.mark.parametrize("above", [12, 17, 24])
+def test_what_lies_far_below_a_sink(ctx, G, T, dtype, above):
+    """A first key that takes nearly all of the weight and has no value: out is what is left of the others, `above` nats below it."""
+    for D, N in ((128, 1100), (64, 2000)):
+        q, k, v = _randn((2, G, T, D), above, dtype), _randn((2, N, D), above + 1, dtype), _randn((2, N, D), above + 2, dtype, 1024.0)
+        q[..., 0], k[:, :, 0], v[:, 0] = 4.0, 0.0, 0.0
+        k[:, 0] = 0.0
+        k[:, 0, 0] = above * math.sqrt(D) / 4
+        _attend(ctx, q, k, v, [N, N - 333])
+
+
+@pytest.mark.parametrize("G,T", QUERIES)
+@pytest.mark.parametrize("dtype", [BF, HF])
+@pytest.mark.parametrize("scale", [8.0, 60.0])
+def test_sharp_logits_and_references_that_move(ctx, G, T, dtype, scale):
+    """Logits of standard deviations up to 60, and the same growing along the row by as much, so that the largest come last."""
+    D, N = 128, 1500
+    q, k, v = _randn((2, G, T, D), 5, dtype, scale), _randn((2, N, D), 6, dtype), _randn((2, N, D), 7, dtype)
+    q[..., 0] = scale
+    k[1, :, 0] = torch.linspace(0, 50, N).to(dtype)
+    _attend(ctx, q, k, v, [N - 200, N])
