@@ -241,7 +241,7 @@ int proxykv_compact_pooled(proxykv_ctx* ctx, void* k, void* v, const int32_t* fl
  *   out [rows, group, T, D]
  *   weight [rows, N] fp32  an account of attention, or NULL: see below
  * New token t sees the row's tokens n < lens - T + 1 + t; probabilities are the softmax of <q, k> / sqrt(D) over them, and out their sum
- * of v.  A query that sees nothing (an empty row, or more new tokens than the row has) gets zeros.  Whatever lies in k, v and
+ * of v.  A query that sees nothing (an empty row, more new tokens than the row has, or nothing but logits of -infinity) gets zeros.  Whatever lies in k, v and
  * weight behind a row's tokens is not used, and weight there is left as it was; a token that only some of the T queries see does not touch
  * the others, NaN and infinities in it included.
  * weight[r, n] += the sum of the probabilities that token n gets from the row's group * T queries: over a decode, how much of the

@@ -3,7 +3,7 @@
 //
 // Three steps.  attend_wave_kernel and, for more than 32 queries per key, attend_block_kernel: waves take shares of a row's keys (a row's new tokens
 // are few, its keys many) and leave, for each query, the share's reference m, its sum l of 2^(c s - m), c = log2(e) / sqrt(D), and its unscaled
-// output, in fp32.  attend_finish_kernel: shares are joined, in order, and where the logits were kept, every key's probabilities are added to the
+// output, in fp32, m as a logit.  attend_finish_kernel: shares are joined, in order, and where the logits were kept, every key's probabilities are added to the
 // account.  attend_account_kernel: where they were not (many queries), they are computed once more.  Rows of few keys go through
 // attend_row_kernel, which does all of it.  No sum's order depends on timing.
 //
@@ -16,9 +16,13 @@
 namespace pkv {
 namespace {
 
-constexpr float kLog2e = 1.4426950408889634f;
+template <int D>
+constexpr float kScale = 1.4426950408889634f / (D == 64 ? 8.0f : 11.313708498984761f);  // of logits, for exponents of 2
 constexpr float kNegInf = -__builtin_huge_valf();
-constexpr float kLow = -1.0e30f;        // a reference below every logit that counts
+constexpr float kLow = -3.4028235e38f;  // the reference of no logits: none lies below
+// Up to here an exponent c s - m is one fma, m a scaled reference or log-sum-exp: rounding m leaves 2^-13 of a probability at most.  Beyond, it
+// would soon leave whole powers of 2, and the exponent is that of a difference of logits, c (s - r).
+constexpr float kFar = 4096.0f;
 constexpr int kTile = 32;               // keys per step of a wave
 constexpr int kXcds = 8;
 constexpr int kMerge = 4;               // waves that are joined in LDS
@@ -93,9 +97,16 @@ struct Plan {
   bool one_launch; // few keys: attend_row_kernel
   float* ml;       // [splits, queries] pairs
   float* o;        // [splits, queries, D]
-  float* lse;      // [queries] in the order of q, and behind them in the shared keys' order
+  float* lse;      // [queries] log2(sum 2^(c s)) in the order of q, and behind them in the shared keys' order
+  float2* parts;   // the same, as a reference and log2 of the sum by it
   float* part_sums;  // accounts of parts of the queries
 };
+
+// A query's reference (a logit), the sum of probabilities by it, and its log2; of nothing +infinity, by which nothing gets a probability.
+struct Joined {
+  float ref, l, log2;
+};
+__device__ __forceinline__ float log2_of(float l) { return l == 0.0f ? -kNegInf : __builtin_amdgcn_logf(l); }
 
 // Where query m of a row's m queries lies in q.  Shared keys: row = head, queries (sequence, group head, token).
 __device__ __forceinline__ int64_t query_at(bool shared, int64_t row, int m, int per, int64_t heads) {
@@ -139,16 +150,16 @@ struct Part {
   static constexpr int MINE = 2 * NL / W;                      // loads of a wave per stage
   static_assert(MINE * W == 2 * NL, "the waves share a stage's loads");
 
-  // WHOLE: the share is all of a row, whose outputs are written and whose queries' log-sum-exps and sums are left in `fin`.
+  // WHOLE: the share is all of a row, whose outputs are written and whose queries' references and sums are left in `fin`.
   template <bool WHOLE = false>
   static __device__ __forceinline__ void run(const AttendArgs& a, const Plan& p, const Keys& ks, bool shared, int64_t row, int split, int tile0, u32x4* lds,
-                                             float2* fin = nullptr) {
+                                             Joined* fin = nullptr) {
     const int lane = threadIdx.x & 63, wave = W == 1 ? 0 : __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), col = lane & 15, quad = lane >> 4;
     const int member = V == 1 ? 0 : __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     lds += member * (STAGES * STAGE);
     const int per = (int)(a.group * a.T), T = (int)a.T, M = (int)ks.m;
     const int b0 = tile0 * 16 * CT * W, m0 = b0 + wave * 16 * CT;
-    const float c = kLog2e / __builtin_sqrtf((float)D);
+    constexpr float c = kScale<D>;
     const int len = row_len(shared ? a.shared_lens : a.lens, row, ks.n);
     // keys that all, and that any, of the block's queries see
     int64_t query[CT];
@@ -171,7 +182,8 @@ struct Part {
     const int begin = begin0 + member * mine, end = begin + mine < end0 ? begin + mine : end0;
     const int n_stages = end > begin ? (end - begin + KEYS - 1) / KEYS : 0;
 
-    float m_run[CT], l_run[CT];
+    float m_run[CT], l_run[CT];  // (references are scaled, unless `far`)
+    bool far = false;
     f32x4 o[DT][CT];
 #pragma unroll
     for (int ct = 0; ct < CT; ++ct) {
@@ -241,19 +253,41 @@ struct Part {
         bool much = false;
 #pragma unroll
         for (int ct = 0; ct < CT; ++ct) much = much || !(sum[ct] <= E::kMostSum);
-        if (__builtin_expect(__builtin_amdgcn_ballot_w64(much) != 0, 0)) {
+        if (__builtin_expect(far || __builtin_amdgcn_ballot_w64(much) != 0, 0)) {
+          float top[CT];
+          bool huge = false;
 #pragma unroll
           for (int ct = 0; ct < CT; ++ct) {
-            float top = max3f(s[0][ct][0], s[0][ct][1], s[0][ct][2]);
-            top = max3f(top, s[0][ct][3], s[1][ct][0]);
-            top = max3f(top, s[1][ct][1], s[1][ct][2]);
-            top = quads_max(__builtin_fmaxf(top, s[1][ct][3])) * c;
-            const float m = __builtin_fmaxf(m_run[ct], top - E::kBelow), f = __builtin_amdgcn_exp2f(m_run[ct] - m);
-            m_run[ct] = m;
+            top[ct] = max3f(s[0][ct][0], s[0][ct][1], s[0][ct][2]);
+            top[ct] = max3f(top[ct], s[0][ct][3], s[1][ct][0]);
+            top[ct] = max3f(top[ct], s[1][ct][1], s[1][ct][2]);
+            top[ct] = quads_max(__builtin_fmaxf(top[ct], s[1][ct][3]));
+            huge = huge || (__builtin_fabsf(top[ct]) * c > kFar && top[ct] != kNegInf);
+          }
+          const bool was = far;
+          far = was || __builtin_amdgcn_ballot_w64(huge) != 0;
+#pragma unroll
+          for (int ct = 0; ct < CT; ++ct) {
+            float f;
+            if (far) {
+              const float old = was ? m_run[ct] : m_run[ct] * (1.0f / c), r = max3f(old, top[ct] - E::kBelow / c, kLow);
+              f = __builtin_amdgcn_exp2f(was ? (old - r) * c : __builtin_fmaf(-r, c, m_run[ct]));
+              m_run[ct] = r;
+              sum[ct] = 0.0f;
+#pragma unroll
+              for (int i = 0; i < 8; ++i) {
+                pf[ct][i] = __builtin_amdgcn_exp2f((s[i >> 2][ct][i & 3] - r) * c);
+                sum[ct] += pf[ct][i];
+              }
+            } else {
+              const float m = __builtin_fmaxf(m_run[ct], top[ct] * c - E::kBelow);
+              f = __builtin_amdgcn_exp2f(m_run[ct] - m);
+              m_run[ct] = m;
+              sum[ct] = probabilities(s, ct, pf[ct]);
+            }
             l_run[ct] *= f;
 #pragma unroll
             for (int d = 0; d < DT; ++d) o[d][ct] *= f;
-            sum[ct] = probabilities(s, ct, pf[ct]);
           }
         }
 #pragma unroll
@@ -498,16 +532,23 @@ struct Part {
         stages(full, n_stages, std::integral_constant<bool, true>{});
       }
     }
+    float own[CT];  // from here on references are logits; what rounding them leaves
+#pragma unroll
+    for (int ct = 0; ct < CT; ++ct) {
+      const float r = far ? m_run[ct] : __builtin_fmaxf(m_run[ct] * (1.0f / c), kLow);
+      own[ct] = far ? 1.0f : __builtin_amdgcn_exp2f(__builtin_fmaf(-r, c, m_run[ct]));
+      m_run[ct] = r;
+    }
     const size_t at = (size_t)(ks.first_split + split) * p.queries;
     if constexpr (V == 1) {
 #pragma unroll
       for (int ct = 0; ct < CT; ++ct) {
-        const float l = quads_sum(l_run[ct]);
+        const float l = quads_sum(l_run[ct]) * own[ct];
         if (m0 + ct * 16 + col < M) {
           if (quad == 0) reinterpret_cast<float2*>(p.ml)[at + query[ct]] = float2{m_run[ct], l};
           if (n_stages > 0) {
 #pragma unroll
-            for (int d = 0; d < DT; ++d) *reinterpret_cast<f32x4*>(p.o + (at + query[ct]) * D + d * 16 + quad * 4) = o[d][ct];
+            for (int d = 0; d < DT; ++d) *reinterpret_cast<f32x4*>(p.o + (at + query[ct]) * D + d * 16 + quad * 4) = o[d][ct] * own[ct];
           }
         }
       }
@@ -521,7 +562,7 @@ struct Part {
       float l_own[CT];
 #pragma unroll
       for (int ct = 0; ct < CT; ++ct) {
-        l_own[ct] = quads_sum(l_run[ct]);
+        l_own[ct] = quads_sum(l_run[ct]) * own[ct];
         if (quad == 0) ml[member * Q + ct * 16 + col] = float2{m_run[ct], l_own[ct]};
       }
       __syncthreads();
@@ -531,12 +572,12 @@ struct Part {
 #pragma unroll
         for (int v = 0; v < V; ++v) m = __builtin_fmaxf(m, ml[v * Q + ct * 16 + col].x);
 #pragma unroll
-        for (int v = 0; v < V; ++v) l = __builtin_fmaf(ml[v * Q + ct * 16 + col].y, __builtin_amdgcn_exp2f(ml[v * Q + ct * 16 + col].x - m), l);
-        const float f = __builtin_amdgcn_exp2f(m_run[ct] - m);
+        for (int v = 0; v < V; ++v) l = __builtin_fmaf(ml[v * Q + ct * 16 + col].y, __builtin_amdgcn_exp2f((ml[v * Q + ct * 16 + col].x - m) * c), l);
+        const float f = __builtin_amdgcn_exp2f((m_run[ct] - m) * c) * own[ct];
 #pragma unroll
         for (int d = 0; d < DT; ++d) *reinterpret_cast<f32x4*>(all + (member * Q + ct * 16 + col) * LINE + d * 16 + quad * 4) = o[d][ct] * f;
         if (member == 0 && quad == 0) {
-          if constexpr (WHOLE) fin[ct * 16 + col] = float2{m0 + ct * 16 + col >= M || l == 0.0f ? -kNegInf : m + __builtin_amdgcn_logf(l), l};
+          if constexpr (WHOLE) fin[ct * 16 + col] = Joined{m, l, log2_of(m0 + ct * 16 + col < M ? l : 0.0f)};
           else if (m0 + ct * 16 + col < M) reinterpret_cast<float2*>(p.ml)[at + query[ct]] = float2{m, l};
         }
       }
@@ -549,7 +590,7 @@ struct Part {
 #pragma unroll
           for (int v = 1; v < V; ++v) sum += *reinterpret_cast<const f32x4*>(all + (v * Q + q) * LINE + d);
           if constexpr (WHOLE) {
-            const float l = fin[q].y;
+            const float l = fin[q].l;
             const u32x2 r = l == 0.0f ? u32x2{0, 0} : Elem<F16>::narrow4(sum / l);
             if (m0 + q < M) *reinterpret_cast<u32x2*>((uint16_t*)a.out + query_at(shared, row, m0 + q, per, a.heads) * D + d) = r;
           } else if (m0 + q < M) {
@@ -611,6 +652,7 @@ __device__ __forceinline__ void join_outputs(const AttendArgs& a, const Plan& p,
   constexpr int LPR = D / 4, G = 256 / LPR / QB;  // threads per row; shares at a time
   __shared__ float part[256 / LPR][D];
   __shared__ float2 part_ml[256 / LPR];
+  constexpr float c = kScale<D>;
   const int tid = threadIdx.x, g = tid / LPR, at = tid % LPR * 4, per = (int)(a.group * a.T);
   const int64_t mine = (int64_t)block * QB + g / G, query = mine < p.queries ? mine : p.queries - 1;
   float m = kLow, l = 0.0f;
@@ -628,7 +670,7 @@ __device__ __forceinline__ void join_outputs(const AttendArgs& a, const Plan& p,
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       if (s0 + u * G >= p.splits || ml[u].y == 0.0f) continue;
-      const float top = __builtin_fmaxf(m, ml[u].x), f = __builtin_amdgcn_exp2f(m - top), f2 = __builtin_amdgcn_exp2f(ml[u].x - top);
+      const float top = __builtin_fmaxf(m, ml[u].x), f = __builtin_amdgcn_exp2f((m - top) * c), f2 = __builtin_amdgcn_exp2f((ml[u].x - top) * c);
       l = l * f + ml[u].y * f2;
       x = x * f + o[u] * f2;
       m = top;
@@ -641,7 +683,7 @@ __device__ __forceinline__ void join_outputs(const AttendArgs& a, const Plan& p,
     if (g % G != 0) return;
     for (int i = 1; i < G; ++i) {
       const float2 ml = part_ml[g + i];
-      const float top = __builtin_fmaxf(m, ml.x), f = __builtin_amdgcn_exp2f(m - top), f2 = __builtin_amdgcn_exp2f(ml.x - top);
+      const float top = __builtin_fmaxf(m, ml.x), f = __builtin_amdgcn_exp2f((m - top) * c), f2 = __builtin_amdgcn_exp2f((ml.x - top) * c);
       l = l * f + ml.y * f2;
       x = x * f + *reinterpret_cast<const f32x4*>(&part[g + i][at]) * f2;
       m = top;
@@ -652,10 +694,12 @@ __device__ __forceinline__ void join_outputs(const AttendArgs& a, const Plan& p,
   const u32x2 r = none ? u32x2{0, 0} : Elem<F16>::narrow4(x / l);
   *reinterpret_cast<u32x2*>((uint16_t*)a.out + query * D + at) = r;
   if (at == 0 && p.lse != nullptr) {
-    const float v = none ? -kNegInf : m + __builtin_amdgcn_logf(l);
-    p.lse[query] = v;
+    const float2 part = {m, log2_of(l)};
+    const float v = __builtin_fmaf(m, c, part.y);
     const int64_t row = query / per;  // (sequence, head)
-    p.lse[p.queries + (row % a.heads * a.batch + row / a.heads) * per + query % per] = v;
+    const int64_t at_shared = p.queries + (row % a.heads * a.batch + row / a.heads) * per + query % per;
+    p.lse[query] = p.lse[at_shared] = v;
+    p.parts[query] = p.parts[at_shared] = part;
   }
 }
 
@@ -663,8 +707,9 @@ __device__ __forceinline__ void join_outputs(const AttendArgs& a, const Plan& p,
 // the store) that takes 3 us where little is to be done, otherwise bound by reading the logits (256 rows of up to 8192, 34 MB, 12 us with the outputs).
 template <int D, int MQ, int KP>
 __device__ __forceinline__ void account_kept(const AttendArgs& a, const Plan& p, const Keys& ks, bool shared, int b) {
+  constexpr float c = kScale<D>;
   typedef float keys_t __attribute__((ext_vector_type(KP)));
-  __shared__ float lse[MQ];
+  __shared__ float2 parts[MQ];
   const int per = (int)(a.group * a.T), M = (int)ks.m, T = (int)a.T;
   const int blocks = (int)((ks.n + 256 * KP - 1) / (256 * KP)), n = b % blocks * (256 * KP) + threadIdx.x * KP;
   const int64_t row = b / blocks;
@@ -692,19 +737,18 @@ __device__ __forceinline__ void account_kept(const AttendArgs& a, const Plan& p,
     for (int i = g; i < p.splits; i += G) {
       const float2 y = reinterpret_cast<const float2*>(p.ml)[(size_t)i * p.queries + query];
       const float t = __builtin_fmaxf(top, y.x);
-      l = l * __builtin_amdgcn_exp2f(top - t) + y.y * __builtin_amdgcn_exp2f(y.x - t);
+      l = l * __builtin_amdgcn_exp2f((top - t) * c) + y.y * __builtin_amdgcn_exp2f((y.x - t) * c);
       top = t;
     }
 #pragma unroll
     for (int off = G / 2; off; off >>= 1) {
       const float m2 = __shfl_xor(top, off, 64), l2 = __shfl_xor(l, off, 64), t = __builtin_fmaxf(top, m2);
-      l = l * __builtin_amdgcn_exp2f(top - t) + l2 * __builtin_amdgcn_exp2f(m2 - t);
+      l = l * __builtin_amdgcn_exp2f((top - t) * c) + l2 * __builtin_amdgcn_exp2f((m2 - t) * c);
       top = t;
     }
-    if (g == 0) lse[m] = m >= M || l == 0.0f ? -kNegInf : top + __builtin_amdgcn_logf(l);
+    if (g == 0) parts[m] = float2{top, log2_of(m < M ? l : 0.0f)};
   }
   __syncthreads();
-  const float c = kLog2e / __builtin_sqrtf((float)D);
   float sum[KP] = {};
   int t = 0;  // m % T
   static_for<MQ / 4>([&](auto four) __attribute__((always_inline)) {
@@ -712,11 +756,11 @@ __device__ __forceinline__ void account_kept(const AttendArgs& a, const Plan& p,
     if (q >= M) return;
 #pragma unroll
     for (int m = q; m < q + 4; ++m) {
-      const float ref = lse[m];
+      const float2 part = parts[m];
       const int see = m < M ? shared ? len : seen(len, T, t) : 0;
       t = t + 1 == T ? 0 : t + 1;
 #pragma unroll
-      for (int e = 0; e < KP; ++e) sum[e] += n + e < see ? __builtin_amdgcn_exp2f(__builtin_fmaf(s[m][e], c, -ref)) : 0.0f;
+      for (int e = 0; e < KP; ++e) sum[e] += n + e < see ? __builtin_amdgcn_exp2f(__builtin_fmaf(s[m][e] - part.x, c, -part.y)) : 0.0f;
     }
   });
 #pragma unroll
@@ -743,12 +787,12 @@ __global__ __launch_bounds__(64 * kMerge) void attend_row_kernel(AttendArgs a, P
   __shared__ u32x4 lds[kMerge * P::STAGES * P::STAGE];
   const int64_t row = blockIdx.x;
   const int M = (int)p.own.m;
-  __shared__ float2 fin[16];
+  __shared__ Joined fin[16];
   P::template run<true>(a, p, p.own, false, row, 0, 0, lds, fin);
   if (a.weight == nullptr) return;
   // the account, four keys a thread, from the logits that the block has kept
   const int T = (int)a.T, len = row_len(a.lens, row, a.N);
-  const float c = kLog2e / __builtin_sqrtf((float)D);
+  constexpr float c = kScale<D>;
   float* w = a.weight + row * a.N;
   const float* scores = p.own.scores + (size_t)row * M * p.own.score_stride;
   for (int n = threadIdx.x * 4; n < len; n += 64 * kMerge * 4) {
@@ -769,11 +813,11 @@ __global__ __launch_bounds__(64 * kMerge) void attend_row_kernel(AttendArgs a, P
       if (q >= M) return;
 #pragma unroll
       for (int m = q; m < q + 4; ++m) {
-        const float ref = fin[m].x;
+        const float2 part = {fin[m].ref, fin[m].log2};
         const int see = m < M ? seen(len, T, t) : 0;
         t = t + 1 == T ? 0 : t + 1;
 #pragma unroll
-        for (int e = 0; e < 4; ++e) sum[e] += n + e < see ? __builtin_amdgcn_exp2f(__builtin_fmaf(s[m][e], c, -ref)) : 0.0f;
+        for (int e = 0; e < 4; ++e) sum[e] += n + e < see ? __builtin_amdgcn_exp2f(__builtin_fmaf(s[m][e] - part.x, c, -part.y)) : 0.0f;
       }
     });
 #pragma unroll
@@ -790,8 +834,8 @@ __global__ __launch_bounds__(64 * kMerge) void attend_row_kernel(AttendArgs a, P
 // the time and the matrix unit for 34.  Three blocks per compute unit, 1 to 8 parts, and 32 x 32 products with the exponentials spread from step to step
 // took as long (the last at a clock of 2.03 GHz where this has 2.2).
 template <int D, bool F16>
-__global__ __launch_bounds__(256, 2) void attend_account_kernel(AttendArgs a, Keys ks, bool shared, const float* __restrict__ lse, int parts,
-                                                                float* __restrict__ part_sums) {
+__global__ __launch_bounds__(256, 2) void attend_account_kernel(AttendArgs a, Keys ks, bool shared, const float* __restrict__ lse,
+                                                                const float2* __restrict__ lse_parts, int parts, float* __restrict__ part_sums) {
   using E = Elem<F16>;
   constexpr int CPR = D / 8, KK = D / 32, QS = 64, STAGE = QS * CPR + QS / 4, LOADS = QS * CPR / 256;  // queries, 16-byte units and a wave's loads of a step
   __shared__ u32x4 lds[3 * STAGE];
@@ -804,7 +848,7 @@ __global__ __launch_bounds__(256, 2) void attend_account_kernel(AttendArgs a, Ke
   const int len = row_len(shared ? a.shared_lens : a.lens, row, ks.n);
   if (b0 >= len) return;
   const int all = (M + QS - 1) / QS, first = (int)((int64_t)all * part / parts), steps = (int)((int64_t)all * (part + 1) / parts) - first;  // (parts <= all)
-  const float c = kLog2e / __builtin_sqrtf((float)D);
+  constexpr float c = kScale<D>;
   typedef const __attribute__((address_space(1))) void* gptr_t;
   typedef __attribute__((address_space(3))) void* lptr_t;
   // This lane's pieces of a step: query r of it, whose row in q moves on by QS queries: a whole number of sequences and `turn` queries of the next.
@@ -882,10 +926,13 @@ __global__ __launch_bounds__(256, 2) void attend_account_kernel(AttendArgs a, Ke
   int stage = 0;
   for (int t = 0; t < steps; ++t) {
     landed(t);
+    const u32x4* st = lds + stage * STAGE;
+    const float some = __builtin_fabsf(reinterpret_cast<const float*>(st + QS * CPR)[lane]);  // (this wave's own load)
+    asm volatile("" ::: "memory");
     __builtin_amdgcn_s_barrier();  // everyone's has, and everyone has read step t - 1, whose place takes step t + 2
     asm volatile("" ::: "memory");
     if (t + 2 < steps) fetch(stage == 0 ? 2 : stage - 1);
-    const u32x4* st = lds + stage * STAGE;
+    const bool far = __builtin_amdgcn_ballot_w64(some > kFar && some != -kNegInf) != 0;  // some of the step's queries have logits far from 0
     const f32x4* refs = reinterpret_cast<const f32x4*>(st + QS * CPR) + quad;
     // whether all the step's queries see all of this wave's keys
     const int q0 = (first + t) * QS, q1 = q0 + QS - 1;
@@ -911,9 +958,11 @@ __global__ __launch_bounds__(256, 2) void attend_account_kernel(AttendArgs a, Ke
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
             const int m = q0 + u * 16 + quad * 4 + e, see = m >= M ? 0 : shared ? len : seen(len, T, remainder_of(m, T, inv_T));
+            float2 part = {0.0f, 0.0f};
+            if (far) part = lse_parts[row * M + (m < M ? m : M - 1)];
 #pragma unroll
             for (int kt = 0; kt < 4; ++kt) {
-              const float y = __builtin_amdgcn_exp2f(__builtin_fmaf(x[cur].s[kt][e], c, -x[cur].ref[e]));
+              const float y = __builtin_amdgcn_exp2f(far ? __builtin_fmaf(x[cur].s[kt][e] - part.x, c, -part.y) : __builtin_fmaf(x[cur].s[kt][e], c, -x[cur].ref[e]));
               sum[kt] += n0 + kt * 16 + col < see ? y : 0.0f;
             }
           }
@@ -931,7 +980,7 @@ __global__ __launch_bounds__(256, 2) void attend_account_kernel(AttendArgs a, Ke
       });
     };
     const int any = shared ? len : seen(len, T, t0 + QS <= T ? t0 + QS - 1 : T - 1);  // keys that some of the step's queries see
-    if (__builtin_expect(q1 < M && n0 + 64 <= least, 1)) work(std::integral_constant<bool, false>{});
+    if (__builtin_expect(q1 < M && n0 + 64 <= least && !far, 1)) work(std::integral_constant<bool, false>{});
     else if (n0 < any) work(std::integral_constant<bool, true>{});
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
     stage = stage == 2 ? 0 : stage + 1;
@@ -1046,6 +1095,7 @@ Plan plan_of(const AttendArgs& a, uint8_t* scratch) {
   p.ml = take((size_t)p.splits * p.queries * 2);
   p.o = take((size_t)p.splits * p.queries * a.D);
   p.lse = take((size_t)p.queries * 2);
+  p.parts = (float2*)take((size_t)p.queries * 4);
   const size_t sums_shared = p.shared.parts > 1 ? (size_t)(p.shared.parts * p.shared.rows * p.shared.n) : 0;
   const size_t sums_own = p.own.parts > 1 ? (size_t)(p.own.parts * p.own.rows * p.own.n) : 0;
   p.part_sums = take(sums_shared > sums_own ? sums_shared : sums_own);
@@ -1106,18 +1156,18 @@ hipError_t launch_attend_of(const AttendArgs& a, void* scratch, hipStream_t stre
   else if (p.splits <= 8) finish_of(std::integral_constant<int, 4>{});
   else finish_of(std::integral_constant<int, 1>{});
   e = hipGetLastError();
-  auto account = [&](const Keys& k, bool shared, float* weight, const int32_t* lens, const float* lse) {
+  auto account = [&](const Keys& k, bool shared, float* weight, const int32_t* lens) {
     if (e != hipSuccess || weight == nullptr || k.n == 0 || k.scores) return;
-    const int64_t blocks = k.rows * ((k.n + 255) / 256);
-    attend_account_kernel<D, F16><<<(unsigned)(blocks * k.parts), 256, 0, stream>>>(a, k, shared, lse, k.parts, p.part_sums);
+    const int64_t blocks = k.rows * ((k.n + 255) / 256), first = shared ? p.queries : 0;
+    attend_account_kernel<D, F16><<<(unsigned)(blocks * k.parts), 256, 0, stream>>>(a, k, shared, p.lse + first, p.parts + first, k.parts, p.part_sums);
     e = hipGetLastError();
     if (e == hipSuccess && k.parts > 1) {
       attend_add_kernel<<<(unsigned)blocks, 256, 0, stream>>>(weight, p.part_sums, lens, k.rows, k.n, k.parts);
       e = hipGetLastError();
     }
   };
-  account(p.shared, true, a.weight_shared, a.shared_lens, p.lse + p.queries);
-  account(p.own, false, a.weight, a.lens, p.lse);
+  account(p.shared, true, a.weight_shared, a.shared_lens);
+  account(p.own, false, a.weight, a.lens);
   return e;
 }
 
@@ -1143,7 +1193,7 @@ size_t attend_scratch_bytes(const AttendArgs& a) {
   shares(rows, a.N, per, a.weight != nullptr);
   shares(a.heads, a.P, a.batch * per, a.weight_shared != nullptr);
   if (a.batch * per > kKeptQueries) shares(a.heads, a.P, kKeptQueries, a.weight_shared != nullptr);  // a smaller batch
-  return (size_t)(outputs * (a.D + 2) + scores + sums + queries * 2) * 4 + 6 * 256;
+  return (size_t)(outputs * (a.D + 2) + scores + sums + queries * 6) * 4 + 7 * 256;
 }
 
 hipError_t launch_attend(const AttendArgs& a, void* scratch, hipStream_t stream) {

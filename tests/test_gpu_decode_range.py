@@ -116,3 +116,34 @@ def test_sharp_logits_and_references_that_move(ctx, G, T, dtype, scale):
     q[..., 0] = scale
     k[1, :, 0] = torch.linspace(0, 50, N).to(dtype)
     _attend(ctx, q, k, v, [N - 200, N])
+
+
+# ---- logits far from zero -------------------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("G,T", QUERIES)
+@pytest.mark.parametrize("sign", [1, -1])
+@pytest.mark.parametrize("dtype,a,b", [(BF, 1, 3), (BF, 4, 5), (BF, 10, 12), (BF, 20, 25), (BF, 55, 60), (HF, 3, 4), (HF, 13, 12)])
+def test_logits_far_from_zero(ctx, G, T, dtype, a, b, sign):
+    """Logits that are whole multiples of 2^(a + b), up to 2^123 and down to -2^123, which fp32 sums hold exactly: the largest have all of the weight, in equal
+    shares.  Every third query is small and has ordinary ones.
+    A difference of logits is exact, its exponent (at most 2^7 where it counts) rounded once, and so is a log-sum-exp of less than 2^12: ln 2 times
+    2^-17 and 2^-13 of a probability in the account."""
+    for D, N in ((128, 700), (64, 333)):
+        g = torch.Generator().manual_seed(a + b)
+        q, k = torch.randint(-1, 2, (2, G, T, D), generator=g).float(), torch.randint(-1, 2, (2, N, D), generator=g).float()
+        q[..., :D // 2], k[..., :D // 2] = 2.0 * sign, 2.0
+        q, k = q * 2.0 ** a, k * 2.0 ** b
+        q.view(2, G * T, D)[:, ::3] *= 2.0 ** (-a - b - 4)
+        q, k, v = q.to(dtype), k.to(dtype), _randn((2, N, D), a, dtype)
+        for account in (True, False):
+            lens = torch.tensor([N, N - 70], dtype=torch.int32)
+            w = torch.zeros(2, N, device="cuda") if account else None
+            out = pk.proxykv_attend(ctx, q.cuda(), k.cuda(), v.cuda(), lens=lens.cuda(), weight=w)
+            torch.cuda.synchronize()
+            ref, w_ref, _, spread = oracle.attend(q[None], k[None], v[None], lens[None])
+            half = torch.finfo(dtype).eps / 2
+            rel = 2 * (2.0 ** -17 + 2.0 ** -22) + (N / 16 + 64) * U
+            least = 2.0 ** -25 + N * 2.0 ** -25 * float(v.abs().max()) if dtype == HF else 0.0  # (far from zero, 11 less than a logit is that logit)
+            _within(out, ref[0], spread[0] * (rel + half ** 2 * 1.01) + half * (1 + 2.0 ** -8) * ref[0].abs() + least, "out")
+            if account:
+                _within(w, w_ref[0], w_ref[0] * (rel + 2.0 ** -13 + (G * T + 2) * U) + G * T * 2.0 ** -126, "weight")
