@@ -39,9 +39,12 @@ struct Elem {
   }
   static constexpr uint32_t kExp = F16 ? 0x7c00u : 0x7f80u;  // all ones: not finite
   static constexpr uint32_t kOne = F16 ? 0x3c00u : 0x3f80u;
-  // Probabilities are relative to their query's reference, which lies kBelow under the largest logit (base 2) whenever it moves; it moves when a
-  // lane's eight come to more than kMostSum.  fp16 has steps of 2^-24 at its low end, so its largest ones begin at 2^11: 2^-36 of that is left.
-  static constexpr float kBelow = F16 ? 11.0f : 0.0f, kMostSum = F16 ? 32768.0f : 4096.0f;
+  // Probabilities are relative to their query's reference, which moves so that the largest is 2^kTop.
+  // fp16: when a lane's eight come to more than kMost.  Its steps are 2^-24 at the low end, 2^-36 of the largest then.
+  // bf16: when all of a lane's so far do, to where those are no more than 2^kSum: a query's in four waves are less than 1, and its output no larger
+  // than its values, which may be as large as fp32 holds.  (From 2^-13 to 2^-5 a move is rare; with 2^-9 and 2^-12 for the largest, 512 new tokens on 10 343
+  // keys took 140 to 145 us in the blocks of eight waves, 136 so.)
+  static constexpr float kTop = F16 ? 11.0f : -16.0f, kSum = -13.0f, kMost = F16 ? 32768.0f : 0.03125f;
   static __device__ __forceinline__ f32x4 mfma(u32x4 a, u32x4 b, f32x4 c) {
     if constexpr (F16) return mfma_f16_16x16x32(as_f16x8(a), as_f16x8(b), c);
     else return mfma_bf16_16x16x32(as_bf16x8(a), as_bf16x8(b), c);
@@ -238,7 +241,7 @@ struct Part {
 #pragma unroll
             for (int ct = 0; ct < CT; ++ct) s[kt][ct] = E::mfma(f[kt][kk], bq[ct][kk], s[kt][ct]);
       };
-      // Probabilities by the reference that there is; only where a lane's come to more than kMostSum are the logits' maxima taken, the
+      // Probabilities by the reference that there is; only where a lane's come to more than kMost are the logits' maxima taken, the
       // reference moved and the probabilities computed again (at first always).
       auto probabilities = [&](const f32x4 (&s)[2][CT], int ct, float (&pf)[8]) __attribute__((always_inline)) {
         float sum = 0.0f;
@@ -252,7 +255,7 @@ struct Part {
       auto keep_reference = [&](const f32x4 (&s)[2][CT], float (&pf)[CT][8], float (&sum)[CT]) __attribute__((always_inline)) {
         bool much = false;
 #pragma unroll
-        for (int ct = 0; ct < CT; ++ct) much = much || !(sum[ct] <= E::kMostSum);
+        for (int ct = 0; ct < CT; ++ct) much = much || !((F16 ? sum[ct] : l_run[ct] + sum[ct]) <= E::kMost);
         if (__builtin_expect(far || __builtin_amdgcn_ballot_w64(much) != 0, 0)) {
           float top[CT];
           bool huge = false;
@@ -268,9 +271,10 @@ struct Part {
           far = was || __builtin_amdgcn_ballot_w64(huge) != 0;
 #pragma unroll
           for (int ct = 0; ct < CT; ++ct) {
+            const float up = F16 ? 0.0f : __builtin_fmaxf(__builtin_amdgcn_logf(quads_max(l_run[ct])) - E::kSum, 0.0f);  // (log2)
             float f;
             if (far) {
-              const float old = was ? m_run[ct] : m_run[ct] * (1.0f / c), r = max3f(old, top[ct] - E::kBelow / c, kLow);
+              const float old = was ? m_run[ct] : m_run[ct] * (1.0f / c), r = max3f(old + up / c, top[ct] - E::kTop / c, kLow);
               f = __builtin_amdgcn_exp2f(was ? (old - r) * c : __builtin_fmaf(-r, c, m_run[ct]));
               m_run[ct] = r;
               sum[ct] = 0.0f;
@@ -280,7 +284,7 @@ struct Part {
                 sum[ct] += pf[ct][i];
               }
             } else {
-              const float m = __builtin_fmaxf(m_run[ct], top[ct] * c - E::kBelow);
+              const float m = __builtin_fmaxf(m_run[ct] + up, top[ct] * c - E::kTop);
               f = __builtin_amdgcn_exp2f(m_run[ct] - m);
               m_run[ct] = m;
               sum[ct] = probabilities(s, ct, pf[ct]);
@@ -655,6 +659,7 @@ __device__ __forceinline__ void join_outputs(const AttendArgs& a, const Plan& p,
   constexpr float c = kScale<D>;
   const int tid = threadIdx.x, g = tid / LPR, at = tid % LPR * 4, per = (int)(a.group * a.T);
   const int64_t mine = (int64_t)block * QB + g / G, query = mine < p.queries ? mine : p.queries - 1;
+  const float down = (float)__builtin_clz(p.splits) - 32.0f;  // each share 2^down of what it has: their sum is finite where every one is
   float m = kLow, l = 0.0f;
   f32x4 x = {0, 0, 0, 0};
   constexpr int U = 4;
@@ -670,7 +675,7 @@ __device__ __forceinline__ void join_outputs(const AttendArgs& a, const Plan& p,
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       if (s0 + u * G >= p.splits || ml[u].y == 0.0f) continue;
-      const float top = __builtin_fmaxf(m, ml[u].x), f = __builtin_amdgcn_exp2f((m - top) * c), f2 = __builtin_amdgcn_exp2f((ml[u].x - top) * c);
+      const float top = __builtin_fmaxf(m, ml[u].x), f = __builtin_amdgcn_exp2f((m - top) * c), f2 = __builtin_amdgcn_exp2f(__builtin_fmaf(ml[u].x - top, c, down));
       l = l * f + ml[u].y * f2;
       x = x * f + o[u] * f2;
       m = top;
@@ -694,7 +699,7 @@ __device__ __forceinline__ void join_outputs(const AttendArgs& a, const Plan& p,
   const u32x2 r = none ? u32x2{0, 0} : Elem<F16>::narrow4(x / l);
   *reinterpret_cast<u32x2*>((uint16_t*)a.out + query * D + at) = r;
   if (at == 0 && p.lse != nullptr) {
-    const float2 part = {m, log2_of(l)};
+    const float2 part = {m, log2_of(l) - down};
     const float v = __builtin_fmaf(m, c, part.y);
     const int64_t row = query / per;  // (sequence, head)
     const int64_t at_shared = p.queries + (row % a.heads * a.batch + row / a.heads) * per + query % per;

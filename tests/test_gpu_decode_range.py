@@ -79,6 +79,15 @@ def test_values_of_every_size_are_kept(ctx, G, T, dtype, scale):
 
 
 @pytest.mark.parametrize("G,T", QUERIES)
+@pytest.mark.parametrize("dtype,scale", [(BF, 2.0 ** 127), (HF, 2.0 ** 15)])
+@pytest.mark.parametrize("N", [130, 3000, 20000])
+def test_the_largest_values_that_there_are(ctx, G, T, dtype, scale, N):
+    """Values near the type's largest, all of one sign: their average is finite, and so is everything on the way to it."""
+    v = ((1.0 + 0.9 * torch.rand(1, N, 64, generator=torch.Generator().manual_seed(N))) * scale).to(dtype)
+    _attend(ctx, _randn((1, G, T, 64), 1, dtype, 0.0 if T % 2 else 2.0), _randn((1, N, 64), 2, dtype), v)
+
+
+@pytest.mark.parametrize("G,T", QUERIES)
 @pytest.mark.parametrize("dtype", [BF, HF])
 def test_probabilities_are_not_one_16_bit_value(ctx, G, T, dtype):
     """Two keys of nearly the same logit with opposite values among keys without any: out is the difference of two probabilities, to the bits of both."""
