@@ -243,7 +243,7 @@ int proxykv_compact_pooled(proxykv_ctx* ctx, void* k, void* v, const int32_t* fl
  * New token t sees the row's tokens n < lens - T + 1 + t; probabilities are the softmax of <q, k> / sqrt(D) over them, and out their sum
  * of v.  A query that sees nothing (an empty row, more new tokens than the row has, or nothing but logits of -infinity) gets zeros.  Whatever lies in k, v and
  * weight behind a row's tokens is not used, and weight there is left as it was; a token that only some of the T queries see does not touch
- * the others, NaN and infinities in it included.
+ * the others, NaN and infinities in it included.  A value of plus or minus infinity that is seen is that in out, both are a NaN.
  * weight[r, n] += the sum of the probabilities that token n gets from the row's group * T queries: over a decode, how much of the
  * attention every cached token has had, by which proxykv_evict selects.  The caller clears it for new tokens.
  * Products of q and k run on MFMA with fp32 accumulation, softmax in fp32; for the product with v a probability is the sum of two values of the

@@ -408,6 +408,49 @@ struct Part {
           }
         }
       };
+      // Behind the whole tiles, in which an infinite value meets the two parts of a probability, of which the second may be 0 or negative, so that any
+      // output that is not finite may have come of one: it is what the row's first `keys` values of its feature say, which all queries see.
+      auto infinite = [&](int keys) __attribute__((always_inline)) {
+        float odd = 0.0f;  // or NaN
+#pragma unroll
+        for (int d = 0; d < DT; ++d)
+#pragma unroll
+          for (int ct = 0; ct < CT; ++ct)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) odd = __builtin_fmaf(o[d][ct][e], 0.0f, odd);
+        if (__builtin_expect(__builtin_amdgcn_ballot_w64(odd != 0.0f) == 0, 1)) return;
+        uint32_t up = 0, down = 0;  // bit 4 d + e: some value of feature 16 d + 4 quad + e is infinite upwards, downwards (a NaN is both)
+#pragma unroll 1
+        for (int n = col; n < keys; n += 16)
+#pragma unroll
+          for (int d = 0; d < DT; ++d) {
+            const u32x2 x = *reinterpret_cast<const u32x2*>(vb + (size_t)n * (D * 2) + d * 32 + quad * 8);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              const uint32_t v = x[e >> 1] >> (e & 1) * 16 & 0xffffu;
+              const bool not_finite = (v & E::kExp) == E::kExp;
+              up |= not_finite && v != (E::kExp | 0x8000u) ? 1u << (4 * d + e) : 0u;
+              down |= not_finite && v != E::kExp ? 1u << (4 * d + e) : 0u;
+            }
+          }
+#pragma unroll
+        for (int off = 1; off < 16; off *= 2) {
+          up |= (uint32_t)__shfl_xor((int)up, off, 64);
+          down |= (uint32_t)__shfl_xor((int)down, off, 64);
+        }
+#pragma unroll
+        for (int ct = 0; ct < CT; ++ct) {
+          const float l = quads_sum(l_run[ct]);
+          if (l != l) continue;  // (a logit that is not a number: nor is any output)
+#pragma unroll
+          for (int d = 0; d < DT; ++d)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              const bool u = up >> (4 * d + e) & 1u, w = down >> (4 * d + e) & 1u;
+              o[d][ct][e] = u && w ? __builtin_nanf("") : u ? -kNegInf : w ? kNegInf : o[d][ct][e];
+            }
+        }
+      };
       // A wave alone has two stages under way; waves that share them ask for the next one when all of them have read the one before.
       // (The waits are on every path: it is where the compiler knows that the queries have landed, for which it otherwise waits in every
       // stage, and for the stages under way with them.)
@@ -529,10 +572,12 @@ struct Part {
           step(f, st + NL * 64 + TILE, sb, sa, std::integral_constant<bool, false>{}, []() {});
           ++done;
           asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+          infinite(full * KEYS);
         }
         stages(done, n_stages, std::integral_constant<bool, true>{});
       } else {
         stages(0, full, std::integral_constant<bool, false>{});
+        if (full > 0) infinite(full * KEYS);
         stages(full, n_stages, std::integral_constant<bool, true>{});
       }
     }

@@ -156,3 +156,49 @@ def test_logits_far_from_zero(ctx, G, T, dtype, a, b, sign):
             _within(out, ref[0], spread[0] * (rel + half ** 2 * 1.01) + half * (1 + 2.0 ** -8) * ref[0].abs() + least, "out")
             if account:
                 _within(w, w_ref[0], w_ref[0] * (rel + 2.0 ** -13 + (G * T + 2) * U) + G * T * 2.0 ** -126, "weight")
+
+
+# ---- values that are not finite -------------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("G,T", QUERIES)
+@pytest.mark.parametrize("dtype,D", [(BF, 128), (HF, 128), (BF, 64), (HF, 64)])
+@pytest.mark.parametrize("N,at", [(700, 0), (700, 300), (700, 690), (70, 3), (2100, 1030)])
+def test_infinite_values(ctx, G, T, dtype, D, N, at):
+    """A value of plus or minus infinity is that in every output that sees it, wherever it lies; both, or a NaN, are a NaN; all other outputs and the account are
+    as they are without it."""
+    inf, nan = float("inf"), float("nan")
+    q, k, v = _randn((2, G, T, D), 5, dtype), _randn((2, N, D), 6, dtype), _randn((2, N, D), 7, dtype)
+    lens = torch.tensor([N, N - 1], dtype=torch.int32)
+    bad = v.clone()
+    bad[0, at, 3], bad[0, at, 9], bad[0, at, 20] = inf, -inf, nan
+    bad[0, at, 33], bad[0, at + 1, 33] = inf, -inf
+    w = torch.zeros(2, N, device="cuda")
+    out = pk.proxykv_attend(ctx, q.cuda(), k.cuda(), bad.cuda(), lens=lens.cuda(), weight=w)
+    torch.cuda.synchronize()
+    ref, tol, w_ref, w_tol = _bounds(q, k, v, lens)
+    got = out.double().cpu()
+    sees = [(torch.arange(T) + N - T >= x).expand(G, T) for x in (at, at + 1)]
+    for d, hit in ((3, inf), (9, -inf)):
+        assert bool((got[0, :, :, d][sees[0]] == hit).all()), d
+    assert bool(got[0, :, :, 20][sees[0]].isnan().all()) and bool(got[0, :, :, 33][sees[1]].isnan().all())
+    assert bool((got[0, :, :, 33][sees[0] & ~sees[1]] == inf).all())
+    for d in (3, 9, 20, 33):
+        got[0, :, :, d][sees[0]] = ref[0, :, :, d][sees[0]]
+    _within(got, ref, tol, "out")
+    _within(w, w_ref, w_tol, "weight")
+
+
+@pytest.mark.parametrize("B,T", [(1, 1), (7, 1), (12, 1), (40, 1), (20, 3)])
+@pytest.mark.parametrize("dtype", [BF, HF])
+def test_infinite_shared_values(ctx, B, T, dtype):
+    """The same among the shared tokens, in front of every sequence's own."""
+    H, G, D, P, N = 2, 4, 128, 900, 150
+    q, ks, vs = _randn((B, H, G, T, D), 1, dtype), _randn((H, P, D), 2, dtype), _randn((H, P, D), 3, dtype)
+    k, v = _randn((B, H, N, D), 4, dtype), _randn((B, H, N, D), 5, dtype)
+    vs[0, 100, 3], vs[1, 899, 4], v[0, 1, 10, 5] = float("inf"), float("-inf"), float("inf")
+    out = pk.proxykv_attend_shared(ctx, q.cuda(), ks.cuda(), vs.cuda(), k.cuda(), v.cuda())
+    torch.cuda.synchronize()
+    want = torch.zeros(B, H, G, T, D, dtype=torch.float64)
+    want[:, 0, ..., 3], want[:, 1, ..., 4], want[0, 1, ..., 5] = float("inf"), float("-inf"), float("inf")
+    got = out.double().cpu()
+    assert torch.equal(torch.where(got.isfinite(), 0.0, got), want)
