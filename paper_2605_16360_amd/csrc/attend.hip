@@ -1231,8 +1231,8 @@ size_t attend_scratch_bytes(const AttendArgs& a) {
   auto shares = [&](int64_t rows, int64_t n, int64_t m, bool account) {  // bounds of keys_of's choices, each growing in rows, n and m
     if (n == 0) return;
     if (m <= kKeptQueries) {
-      const int64_t s = (n + 383) / 384;
-      outputs += rows * m * (s < kMostSplits ? s : kMostSplits) + kKeptQueries * (1024 + rows);
+      const int64_t s = (n + 383) / 384, many = rows * (s < kMostSplits ? s : kMostSplits), few = rows + 1024;  // (shares of 64 or 128 keys: of up to 2^17 in all)
+      outputs += m * (many > few ? many : few);
       scores += account ? rows * m * ((n + kTile - 1) / kTile * kTile) + 64 : 0;
     } else {
       const int64_t tile = m <= 64 ? 64 : m <= 128 ? 128 : 256;

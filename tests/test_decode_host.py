@@ -127,3 +127,20 @@ def test_sizes_behind_the_largest_are_refused():
                shared(h, 1, 2**16, 2**15, 8, 1, 1), shared(h, 2**8, 2**8, 8, 2**15, 1, 1), evict(h, 2**21, 10, 5, 1), len(launches())]
     """.replace("\n        ", "\n"))
     assert out == [-1] * 7 + [0]
+
+
+def test_workspace_of_many_short_rows():
+    """Two shares of D + 2 fp32 words a query at most, its logits by whole tiles and what it leaves, and 64 MB, however many rows there are: with one query
+    a row it is not that of 32."""
+    sizes = [("attend", (2**20, 16, 1, 1), 2**20, 32), ("attend", (2**18, 16, 4, 1), 2**20, 32), ("attend", (2**16, 100, 8, 2), 2**20, 128),
+             ("shared", (2**12, 2**6, 100, 16, 1, 1), 2**18, 32)]
+    out = run(CALLS + f"""
+out = []
+for name, sizes, queries, logits in {sizes!r}:
+    used = fake.fake_used()
+    h = context(LLAMA)
+    assert globals()[name](h, *sizes) == 0
+    out.append((fake.fake_used() - used) / (queries * (2 * 130 + logits + 6) * 4 + (1 << 26)))
+    kept.clear()
+""")
+    assert all(x <= 1 for x in out), out
