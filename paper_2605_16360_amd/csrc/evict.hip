@@ -309,7 +309,7 @@ __global__ __launch_bounds__(256) void evict_move_kernel(u32x4* __restrict__ k, 
 #pragma unroll
   for (int u = 0; u < kPer; ++u) {
     const int piece = tid + 256 * u;
-    tok[u] = piece < step * cps ? piece / cps : 1 << 30;
+    tok[u] = evict_token(piece, step, cps);
     ch[u] = piece % cps;
   }
   auto load = [&](int j0, u32x4 (&x)[kPer], int (&dst)[kPer]) __attribute__((always_inline)) {  // (a piece behind the end reads the last token's and stores nothing)

@@ -91,6 +91,9 @@ struct AttendArgs {
 size_t attend_scratch_bytes(const AttendArgs& a);
 hipError_t launch_attend(const AttendArgs& a, void* scratch, hipStream_t stream);
 
+// Which token of a step (`step` tokens of cps pieces each) a thread's piece belongs to.  One behind them belongs to none: it stands behind every
+// entry of every row, which has less than 2^31 - 4096 tokens.
+__host__ __device__ inline int evict_token(int piece, int step, int cps) { return piece < step * cps ? piece / cps : 0x7fffffff; }
 // Brings every row of more than `budget` (or budgets[r]) tokens back to it (evict.hip).
 size_t evict_scratch_bytes(int64_t rows, int64_t N);
 hipError_t launch_evict(void* k, void* v, float* weight, int32_t* positions, int32_t* lens, const int32_t* budgets, int64_t rows, int64_t N,

@@ -1,8 +1,10 @@
 """The host side of the decode entry points on a device that is not there (fake_hip.cpp): what they allocate, what they do while a stream
 captures, and that every launch of the largest calls stays within the runtime's limits."""
+import os
 import random
+import subprocess
 
-from test_workspace_host import run
+from test_workspace_host import ROOT, run
 
 CALLS = """
 def attend(h, rows, N, group, T, D=128, dtype=0, weight=True):
@@ -144,3 +146,24 @@ for name, sizes, queries, logits in {sizes!r}:
     kept.clear()
 """)
     assert all(x <= 1 for x in out), out
+
+
+def test_threads_without_a_piece_store_nothing_in_the_longest_row(tmp_path):
+    """A step of eviction's moves has 1024 pieces of 16 bytes; of those that are no whole token no thread may take part, however many entries are left."""
+    (tmp_path / "t.cpp").write_text("""
+#include "kernels.hpp"
+#include <cstdio>
+int main() {
+  const int most = 2147483647 - 4096;  // entries of a row
+  int bad = 0;
+  for (int cps = 1; cps <= 32; ++cps)
+    for (int step = 1024 / cps, piece = 0; piece < 1024; ++piece) {
+      const int t = pkv::evict_token(piece, step, cps);
+      bad += piece < step * cps ? t != piece / cps : t < most;
+    }
+  printf("%d", bad);
+}
+""")
+    subprocess.run(["g++", "-std=c++17", "-D__HIP_PLATFORM_AMD__", "-I/opt/rocm/include", "-I" + os.path.join(ROOT, "paper_2605_16360_amd", "csrc"),
+                    str(tmp_path / "t.cpp"), "-o", str(tmp_path / "t")], check=True)
+    assert subprocess.run([str(tmp_path / "t")], capture_output=True, text=True, check=True).stdout == "0"
