@@ -35,18 +35,22 @@ def _randn(shape, seed, dtype, scale=1.0):
     return (torch.randn(*shape, generator=g) * scale).to(dtype)
 
 
-def _bounds(q, k, v, lens):
-    """(out, weight) of the oracle and what each may be off by, without any allowance that is not relative to what is summed."""
+def _bounds(q, k, v, lens, exact=False):
+    """(out, weight) of the oracle and what each may be off by, without any allowance that is not relative to what is summed.
+    exact: logits far from zero that fp32 sums hold.  A difference of two is exact, its exponent (at most 2^7 where it counts) rounded once, and so is a log-sum-exp
+    of less than 2^12: ln 2 times 2^-17, and 2^-13 of a probability in the account.  (11 less than such a logit may be that logit.)"""
     rows, G, T, D = q.shape
     out, w, _, spread = oracle.attend(q[None], k[None], v[None], lens[None])
     n = k.shape[1]
     mass = (q.double().abs().reshape(rows, G * T, D) @ k.double().abs().transpose(1, 2)).amax((1, 2)).view(rows, 1, 1, 1)
     rel = 2 * (math.log(2) * (2 * D + 8) * U * 1.4427 / math.sqrt(D) * mass + 2.0 ** -22) + (n / 16 + 64) * U
+    if exact:
+        rel = torch.full_like(rel, 2 * (2.0 ** -17 + 2.0 ** -22) + (n / 16 + 64) * U)
     half = torch.finfo(q.dtype).eps / 2
     split = half ** 2 * 1.01
-    least = 2.0 ** -25 + n * 2.0 ** -36 * float(v.abs().max()) if q.dtype == HF else 0.0
+    least = 2.0 ** -25 + n * 2.0 ** (-25 if exact else -36) * float(v.abs().max()) if q.dtype == HF else 0.0
     tol_out = spread[0] * (rel + split) + half * (1 + 2.0 ** -8) * out[0].abs() + least
-    tol_w = w[0] * (rel[:, 0, 0] + (G * T + 2) * U) + G * T * 2.0 ** -126  # (fp32 has no full precision below 2^-126: the smallest of each query's terms may be lost)
+    tol_w = w[0] * (rel[:, 0, 0] + (2.0 ** -13 if exact else 0) + (G * T + 2) * U) + G * T * 2.0 ** -126  # (fp32 has no full precision below 2^-126: the smallest of each query's terms may be lost)
     return out[0], tol_out, w[0], tol_w
 
 
@@ -57,12 +61,12 @@ def _within(got, ref, tol, name):
     assert bool((err <= tol).all()), f"{name}: worst {float((err / tol.clamp_min(1e-300)).max()):.3g} of the bound, max abs err {float(err.max()):.3e}"
 
 
-def _attend(ctx, q, k, v, lens=None, account=True):
+def _attend(ctx, q, k, v, lens=None, account=True, exact=False):
     lens = torch.full((k.shape[0],), k.shape[1], dtype=torch.int32) if lens is None else torch.tensor(lens, dtype=torch.int32)
     w = torch.zeros(k.shape[:2], device="cuda") if account else None
     out = pk.proxykv_attend(ctx, q.cuda(), k.cuda(), v.cuda(), lens=lens.cuda(), weight=w)
     torch.cuda.synchronize()
-    ref, tol, w_ref, w_tol = _bounds(q, k, v, lens)
+    ref, tol, w_ref, w_tol = _bounds(q, k, v, lens, exact)
     _within(out, ref, tol, "out")
     if account:
         _within(w, w_ref, w_tol, "weight")
@@ -134,9 +138,7 @@ def test_sharp_logits_and_references_that_move(ctx, G, T, dtype, scale):
 @pytest.mark.parametrize("dtype,a,b", [(BF, 1, 3), (BF, 4, 5), (BF, 10, 12), (BF, 20, 25), (BF, 55, 60), (HF, 3, 4), (HF, 13, 12)])
 def test_logits_far_from_zero(ctx, G, T, dtype, a, b, sign):
     """Logits that are whole multiples of 2^(a + b), up to 2^123 and down to -2^123, which fp32 sums hold exactly: the largest have all of the weight, in equal
-    shares.  Every third query is small and has ordinary ones.
-    A difference of logits is exact, its exponent (at most 2^7 where it counts) rounded once, and so is a log-sum-exp of less than 2^12: ln 2 times
-    2^-17 and 2^-13 of a probability in the account."""
+    shares.  Every third query is small and has ordinary ones."""
     for D, N in ((128, 700), (64, 333)):
         g = torch.Generator().manual_seed(a + b)
         q, k = torch.randint(-1, 2, (2, G, T, D), generator=g).float(), torch.randint(-1, 2, (2, N, D), generator=g).float()
@@ -145,17 +147,7 @@ def test_logits_far_from_zero(ctx, G, T, dtype, a, b, sign):
         q.view(2, G * T, D)[:, ::3] *= 2.0 ** (-a - b - 4)
         q, k, v = q.to(dtype), k.to(dtype), _randn((2, N, D), a, dtype)
         for account in (True, False):
-            lens = torch.tensor([N, N - 70], dtype=torch.int32)
-            w = torch.zeros(2, N, device="cuda") if account else None
-            out = pk.proxykv_attend(ctx, q.cuda(), k.cuda(), v.cuda(), lens=lens.cuda(), weight=w)
-            torch.cuda.synchronize()
-            ref, w_ref, _, spread = oracle.attend(q[None], k[None], v[None], lens[None])
-            half = torch.finfo(dtype).eps / 2
-            rel = 2 * (2.0 ** -17 + 2.0 ** -22) + (N / 16 + 64) * U
-            least = 2.0 ** -25 + N * 2.0 ** -25 * float(v.abs().max()) if dtype == HF else 0.0  # (far from zero, 11 less than a logit is that logit)
-            _within(out, ref[0], spread[0] * (rel + half ** 2 * 1.01) + half * (1 + 2.0 ** -8) * ref[0].abs() + least, "out")
-            if account:
-                _within(w, w_ref[0], w_ref[0] * (rel + 2.0 ** -13 + (G * T + 2) * U) + G * T * 2.0 ** -126, "weight")
+            _attend(ctx, q, k, v, [N, N - 70], account, exact=True)
 
 
 # ---- values that are not finite -------------------------------------------------------------------------------------
@@ -202,3 +194,43 @@ def test_infinite_shared_values(ctx, B, T, dtype):
     want[:, 0, ..., 3], want[:, 1, ..., 4], want[0, 1, ..., 5] = float("inf"), float("-inf"), float("inf")
     got = out.double().cpu()
     assert torch.equal(torch.where(got.isfinite(), 0.0, got), want)
+
+
+@pytest.mark.parametrize("B,T", [(2, 1), (7, 1), (16, 1), (40, 1), (24, 3)])
+@pytest.mark.parametrize("dtype", [BF, HF])
+@pytest.mark.parametrize("kind", ["sharp", "sink", "small", "far"])
+def test_shared_tokens_in_front_of_own(ctx, B, T, dtype, kind):
+    """Rows of 8 to 288 queries on the shared tokens and of 4 and 12 on a sequence's own: logits that grow to the last own token, a shared sink without a value, small
+    values, and logits far from zero, of which the own ones are as large as the shared."""
+    H, G, D, P, N = 2, 4, 128, 900, 150
+    q, k, v = _randn((B, H, G, T, D), B, dtype), _randn((B, H, P + N, D), B + 1, dtype), _randn((B, H, P + N, D), B + 2, dtype)
+    if kind == "sharp":
+        q = q * 16
+        q[..., 0] = 16.0
+        k[..., 0] = torch.linspace(0, 50, P + N).to(dtype)
+    elif kind == "sink":
+        q[..., 0], k[..., 0] = 4.0, 0.0
+        k[:, :, 0] = 0.0
+        k[:, :, 0, 0] = 17 * math.sqrt(D) / 4
+        v = v * 1024
+        v[:, :, 0] = 0.0
+    elif kind == "small":
+        v = v * 2.0 ** (-27 if dtype == BF else -10)
+    else:
+        g = torch.Generator().manual_seed(B)
+        q, k = torch.randint(-1, 2, q.shape, generator=g).float(), torch.randint(-1, 2, k.shape, generator=g).float()
+        q[..., :64], k[..., :64] = -2.0, 2.0
+        q, k = (q * 2.0 ** 12).to(dtype), (k * 2.0 ** 12).to(dtype)
+    k[:, :, :P], v[:, :, :P] = k[:1, :, :P], v[:1, :, :P]
+    ks, vs, ko, vo = (x.contiguous().cuda() for x in (k[0, :, :P], v[0, :, :P], k[:, :, P:], v[:, :, P:]))
+    w, ws = torch.zeros(B, H, N, device="cuda"), torch.zeros(H, P, device="cuda")
+    out = pk.proxykv_attend_shared(ctx, q.cuda(), ks, vs, ko, vo, weight_shared=ws, weight=w)
+    torch.cuda.synchronize()
+    ref_ws, tol_ws = torch.zeros(H, P, dtype=torch.float64), torch.zeros(H, P, dtype=torch.float64)
+    for b in range(B):
+        ref, tol, w_ref, w_tol = _bounds(q[b], k[b], v[b], torch.full((H,), P + N, dtype=torch.int32), exact=kind == "far")
+        _within(out[b], ref, tol, "out")
+        _within(w[b], w_ref[:, P:], w_tol[:, P:], "weight")
+        ref_ws += w_ref[:, :P]
+        tol_ws += w_tol[:, :P]
+    _within(ws, ref_ws, tol_ws + ref_ws * B * U, "weight_shared")
