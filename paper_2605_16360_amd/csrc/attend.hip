@@ -45,6 +45,7 @@ struct Elem {
   // than its values, which may be as large as fp32 holds.  (From 2^-13 to 2^-5 a move is rare; with 2^-9 and 2^-12 for the largest, 512 new tokens on 10 343
   // keys took 140 to 145 us in the blocks of eight waves, 136 so.)
   static constexpr float kTop = F16 ? 11.0f : -16.0f, kSum = -13.0f, kMost = F16 ? 32768.0f : 0.03125f;
+  static constexpr float kUnit = F16 ? 1.0f / 2048.0f : 65536.0f;  // 2^-kTop: what a wave leaves are a reference near its largest logit, sums by that, and outputs 2^kTop of those
   static __device__ __forceinline__ f32x4 mfma(u32x4 a, u32x4 b, f32x4 c) {
     if constexpr (F16) return mfma_f16_16x16x32(as_f16x8(a), as_f16x8(b), c);
     else return mfma_bf16_16x16x32(as_bf16x8(a), as_bf16x8(b), c);
@@ -185,7 +186,7 @@ struct Part {
     const int begin = begin0 + member * mine, end = begin + mine < end0 ? begin + mine : end0;
     const int n_stages = end > begin ? (end - begin + KEYS - 1) / KEYS : 0;
 
-    float m_run[CT], l_run[CT];  // (references are scaled, unless `far`)
+    float m_run[CT], l_run[CT];  // (a reference is scaled, and kTop less than the logit that gets 2^kTop; if `far`, it is that logit)
     bool far = false;
     f32x4 o[DT][CT];
 #pragma unroll
@@ -274,13 +275,13 @@ struct Part {
             const float up = F16 ? 0.0f : __builtin_fmaxf(__builtin_amdgcn_logf(quads_max(l_run[ct])) - E::kSum, 0.0f);  // (log2)
             float f;
             if (far) {
-              const float old = was ? m_run[ct] : m_run[ct] * (1.0f / c), r = max3f(old + up / c, top[ct] - E::kTop / c, kLow);
-              f = __builtin_amdgcn_exp2f(was ? (old - r) * c : __builtin_fmaf(-r, c, m_run[ct]));
+              const float old = was ? m_run[ct] : (m_run[ct] + E::kTop) * (1.0f / c), r = max3f(old + up / c, top[ct], kLow);
+              f = __builtin_amdgcn_exp2f(was ? (old - r) * c : __builtin_fmaf(-r, c, m_run[ct] + E::kTop));
               m_run[ct] = r;
               sum[ct] = 0.0f;
 #pragma unroll
               for (int i = 0; i < 8; ++i) {
-                pf[ct][i] = __builtin_amdgcn_exp2f((s[i >> 2][ct][i & 3] - r) * c);
+                pf[ct][i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[i >> 2][ct][i & 3] - r, c, E::kTop));
                 sum[ct] += pf[ct][i];
               }
             } else {
@@ -584,15 +585,15 @@ struct Part {
     float own[CT];  // from here on references are logits; what rounding them leaves
 #pragma unroll
     for (int ct = 0; ct < CT; ++ct) {
-      const float r = far ? m_run[ct] : __builtin_fmaxf(m_run[ct] * (1.0f / c), kLow);
-      own[ct] = far ? 1.0f : __builtin_amdgcn_exp2f(__builtin_fmaf(-r, c, m_run[ct]));
+      const float r = far ? m_run[ct] : __builtin_fmaxf((m_run[ct] + E::kTop) * (1.0f / c), kLow);
+      own[ct] = far ? 1.0f : __builtin_amdgcn_exp2f(__builtin_fmaf(-r, c, m_run[ct] + E::kTop));
       m_run[ct] = r;
     }
     const size_t at = (size_t)(ks.first_split + split) * p.queries;
     if constexpr (V == 1) {
 #pragma unroll
       for (int ct = 0; ct < CT; ++ct) {
-        const float l = quads_sum(l_run[ct]) * own[ct];
+        const float l = quads_sum(l_run[ct]) * own[ct] * E::kUnit;
         if (m0 + ct * 16 + col < M) {
           if (quad == 0) reinterpret_cast<float2*>(p.ml)[at + query[ct]] = float2{m_run[ct], l};
           if (n_stages > 0) {
@@ -611,7 +612,7 @@ struct Part {
       float l_own[CT];
 #pragma unroll
       for (int ct = 0; ct < CT; ++ct) {
-        l_own[ct] = quads_sum(l_run[ct]) * own[ct];
+        l_own[ct] = quads_sum(l_run[ct]) * own[ct] * E::kUnit;
         if (quad == 0) ml[member * Q + ct * 16 + col] = float2{m_run[ct], l_own[ct]};
       }
       __syncthreads();
@@ -640,7 +641,7 @@ struct Part {
           for (int v = 1; v < V; ++v) sum += *reinterpret_cast<const f32x4*>(all + (v * Q + q) * LINE + d);
           if constexpr (WHOLE) {
             const float l = fin[q].l;
-            const u32x2 r = l == 0.0f ? u32x2{0, 0} : Elem<F16>::narrow4(sum / l);
+            const u32x2 r = l == 0.0f ? u32x2{0, 0} : E::narrow4(sum / l * E::kUnit);
             if (m0 + q < M) *reinterpret_cast<u32x2*>((uint16_t*)a.out + query_at(shared, row, m0 + q, per, a.heads) * D + d) = r;
           } else if (m0 + q < M) {
             *reinterpret_cast<f32x4*>(p.o + (at + query_at(shared, row, m0 + q, per, a.heads)) * D + d) = sum;
@@ -741,7 +742,7 @@ __device__ __forceinline__ void join_outputs(const AttendArgs& a, const Plan& p,
   }
   if (mine >= p.queries) return;
   const bool none = l == 0.0f;
-  const u32x2 r = none ? u32x2{0, 0} : Elem<F16>::narrow4(x / l);
+  const u32x2 r = none ? u32x2{0, 0} : Elem<F16>::narrow4(x / l * Elem<F16>::kUnit);
   *reinterpret_cast<u32x2*>((uint16_t*)a.out + query * D + at) = r;
   if (at == 0 && p.lse != nullptr) {
     const float2 part = {m, log2_of(l) - down};

@@ -38,7 +38,7 @@ def _randn(shape, seed, dtype, scale=1.0):
 def _bounds(q, k, v, lens, exact=False):
     """(out, weight) of the oracle and what each may be off by, without any allowance that is not relative to what is summed.
     exact: logits far from zero that fp32 sums hold.  A difference of two is exact, its exponent (at most 2^7 where it counts) rounded once, and so is a log-sum-exp
-    of less than 2^12: ln 2 times 2^-17, and 2^-13 of a probability in the account.  (11 less than such a logit may be that logit.)"""
+    of less than 2^12: ln 2 times 2^-17, and 2^-13 of a probability in the account."""
     rows, G, T, D = q.shape
     out, w, _, spread = oracle.attend(q[None], k[None], v[None], lens[None])
     n = k.shape[1]
@@ -48,7 +48,7 @@ def _bounds(q, k, v, lens, exact=False):
         rel = torch.full_like(rel, 2 * (2.0 ** -17 + 2.0 ** -22) + (n / 16 + 64) * U)
     half = torch.finfo(q.dtype).eps / 2
     split = half ** 2 * 1.01
-    least = 2.0 ** -25 + n * 2.0 ** (-25 if exact else -36) * float(v.abs().max()) if q.dtype == HF else 0.0
+    least = 2.0 ** -25 + n * 2.0 ** -36 * float(v.abs().max()) if q.dtype == HF else 0.0
     tol_out = spread[0] * (rel + split) + half * (1 + 2.0 ** -8) * out[0].abs() + least
     tol_w = w[0] * (rel[:, 0, 0] + (2.0 ** -13 if exact else 0) + (G * T + 2) * U) + G * T * 2.0 ** -126  # (fp32 has no full precision below 2^-126: the smallest of each query's terms may be lost)
     return out[0], tol_out, w[0], tol_w
@@ -234,3 +234,13 @@ def test_shared_tokens_in_front_of_own(ctx, B, T, dtype, kind):
         ref_ws += w_ref[:, :P]
         tol_ws += w_tol[:, :P]
     _within(ws, ref_ws, tol_ws + ref_ws * B * U, "weight_shared")
+
+
+@pytest.mark.parametrize("G,T", QUERIES)
+@pytest.mark.parametrize("dtype", [BF, HF])
+def test_the_largest_values_with_logits_far_from_zero(ctx, G, T, dtype):
+    """Both extremes at once, with a logit per query that all keys share."""
+    N, D = 2000, 64
+    q, k = torch.full((1, G, T, D), -2.0 ** 12), torch.full((1, N, D), 2.0 ** 12)
+    v = (1.0 + 0.9 * torch.rand(1, N, D, generator=torch.Generator().manual_seed(2))) * 2.0 ** (127 if dtype == BF else 15)
+    _attend(ctx, q.to(dtype), k.to(dtype), v.to(dtype), exact=True)
