@@ -2,9 +2,9 @@
 // weight that every cached token gets.
 //
 // Three steps.  attend_wave_kernel and, for more than 32 queries per key, attend_block_kernel: waves take shares of a row's keys (a row's new tokens
-// are few, its keys many) and leave, for each query, the share's reference m, its sum l of 2^(c s - m), c = log2(e) / sqrt(D), and its unscaled
-// output, in fp32, m as a logit.  attend_finish_kernel: shares are joined, in order, and where the logits were kept, every key's probabilities are added to the
-// account.  attend_account_kernel: where they were not (many queries), they are computed once more.  Rows of few keys go through
+// are few, its keys many) and leave, for each query, the share's reference m (a logit), its sum l of 2^(c (s - m)), c = log2(e) / sqrt(D), and its
+// output, not divided yet, in fp32.  attend_finish_kernel: shares are joined, in order, and where the logits were kept, every key's probabilities are added
+// to the account.  attend_account_kernel: where they were not (many queries), they are computed once more.  Rows of few keys go through
 // attend_row_kernel, which does all of it.  No sum's order depends on timing.
 //
 // A tile is 32 keys.  S^T = K Q^T on 16 x 16 x 32 matrix instructions: a lane has one query (column) and 8 of the keys, so that a softmax needs
@@ -45,7 +45,8 @@ struct Elem {
   // than its values, which may be as large as fp32 holds.  (From 2^-13 to 2^-5 a move is rare; with 2^-9 and 2^-12 for the largest, 512 new tokens on 10 343
   // keys took 140 to 145 us in the blocks of eight waves, 136 so.)
   static constexpr float kTop = F16 ? 11.0f : -16.0f, kSum = -13.0f, kMost = F16 ? 32768.0f : 0.03125f;
-  static constexpr float kUnit = F16 ? 1.0f / 2048.0f : 65536.0f;  // 2^-kTop: what a wave leaves are a reference near its largest logit, sums by that, and outputs 2^kTop of those
+  // 2^-kTop: a wave leaves a reference near its largest logit, sums by that, and outputs 2^kTop of those
+  static constexpr float kUnit = F16 ? 1.0f / 2048.0f : 65536.0f;
   static __device__ __forceinline__ f32x4 mfma(u32x4 a, u32x4 b, f32x4 c) {
     if constexpr (F16) return mfma_f16_16x16x32(as_f16x8(a), as_f16x8(b), c);
     else return mfma_bf16_16x16x32(as_bf16x8(a), as_bf16x8(b), c);
@@ -665,9 +666,9 @@ __device__ __forceinline__ bool share_of(int b, const Keys& ks, int64_t& row, in
 }
 
 // Few queries per row: V waves for a share of its keys.  CT: of the kind of keys that has the larger tiles.  Bound by reading the cache: 256 rows of up
-// to 8192 keys, 4 queries, 540 MB in 117 us (4.6 TB/s; a large copy reaches 5.2), 8 rows of 10 240 in 10.5.  Waves of their own, five of
+// to 8192 keys, 4 queries, 540 MB in 116 us (4.6 TB/s; a large copy reaches 5.2), 8 rows of 10 240 in 10.5.  Waves of their own, five of
 // which fit a compute unit's LDS, rather than blocks: nothing waits for anything but its own loads.  From 17 queries on what a share leaves is a quarter
-// of what it reads, and four waves are joined first (64 rows of up to 4001 keys of 64, 20 queries: 15 us).
+// of what it reads, and four waves are joined first (64 rows of up to 4001 keys of 64, 20 queries: 16 us).
 template <int D, bool F16, int CT, int V>
 __global__ __launch_bounds__(64 * V, CT == 1 ? 2 : 1) void attend_wave_kernel(AttendArgs a, Plan p) {
   __shared__ u32x4 lds[V * Part<D, F16, CT, 1, V>::STAGES * Part<D, F16, CT, 1, V>::STAGE];
@@ -680,10 +681,13 @@ __global__ __launch_bounds__(64 * V, CT == 1 ? 2 : 1) void attend_wave_kernel(At
   else Part<D, F16, CT, 1, V>::run(a, p, ks, shared, row, split, tile, lds);
 }
 
-// Many: W waves of 32 queries share the keys.  2048 queries on 10 343 keys of 128 for each of 8 heads (W = 8), 8.7e10 flop, take 119 us, 256 on 32 768
-// 51 (0.73 and 0.67 PFLOP/s; a large library product reaches 1.25).  The matrix unit is busy for 37 % of that, and no one thing bounds the rest: without
-// the reads of K out of LDS it would be 17 us less, without those of V 5, without exponentials 8, without the products with V 13.  Half of the waves
-// half a step behind the others were 2 % slower, and orders of products and exponentials or wave priorities made no difference.
+// Many: W waves of 32 queries share the keys.  2048 queries on 10 343 keys of 128 for each of 8 heads (W = 8), 8.7e10 flop and half as many again for the
+// second part of the probabilities, take 139 us, 256 on 32 768 58 (0.94 and 0.89 PFLOP/s with those; a large library product reaches 1.25).  The matrix
+// unit is busy for 48 % of that, and no one thing bounds the rest: without the reads of K out of LDS it would be 4 us less, without those of V 8, without exponentials
+// 12, without the products with the second part 17.  Half of the waves half a step behind the others, and that part worked out between the products
+// with the first, were 2 % slower; other orders of products and exponentials or wave priorities made no difference.
+// W = 2: 64 queries on 10 240 keys of 8 rows 19.9 us, W = 4: 128 queries 22.9, where reading the keys alone takes 8 (they ask for a stage when the one
+// before has landed, and leave 11 and 21 MB of outputs for 42 MB of keys).
 template <int D, bool F16, int W>
 __global__ __launch_bounds__(64 * W, W == 2 ? 1 : 2) void attend_block_kernel(AttendArgs a, Plan p, bool shared) {
   __shared__ u32x4 lds[Part<D, F16, 2, W, 1>::STAGES * Part<D, F16, 2, W, 1>::STAGE];
@@ -696,7 +700,7 @@ __global__ __launch_bounds__(64 * W, W == 2 ? 1 : 2) void attend_block_kernel(At
 
 // Joins the shares' outputs: D / 4 threads hold a share's row, so that a block takes 8 queries of up to four shares (QB = 8), 4 of up to eight, or one
 // query's 256 / (D / 4) shares at a time.  Bound by reading them: 16 384 queries of four shares, 36 MB and 4.5 MB written, 9 us (with QB = 4, where half
-// of the reads are another's share once more, 11.5).
+// of the reads are another's share once more, 12).
 template <int D, bool F16, int QB>
 __device__ __forceinline__ void join_outputs(const AttendArgs& a, const Plan& p, int block) {
   constexpr int LPR = D / 4, G = 256 / LPR / QB;  // threads per row; shares at a time
@@ -831,7 +835,7 @@ __global__ __launch_bounds__(256) void attend_finish_kernel(AttendArgs a, Plan p
 }
 
 // A row of few keys and its queries from beginning to end, in one launch: four waves have a quarter of the keys each and are joined in LDS, and the logits,
-// for the account, come out of the compute unit's own cache.  A chain of waits: 4 rows of up to 512 keys 8.9 us, of 256 6.7.
+// for the account, come out of the compute unit's own cache.  A chain of waits: 4 rows of up to 512 keys 9.1 us, of 256 6.9.
 template <int D, bool F16>
 __global__ __launch_bounds__(64 * kMerge) void attend_row_kernel(AttendArgs a, Plan p) {
   using P = Part<D, F16, 1, 1, kMerge>;
@@ -881,7 +885,7 @@ __global__ __launch_bounds__(64 * kMerge) void attend_row_kernel(AttendArgs a, P
 // them, or one of `parts` parts of those, 64 at a time, through LDS.  S: a lane has the logits of its key (column) with queries 4 quad + r, so
 // that a key's sum stays in the lane until the end.  The products of 16 queries are spread between the exponentials of the 16 before: one
 // after the other, matrix and vector instructions of a SIMD's waves take turns.  Sums of parts are added up by attend_add_kernel.
-// 2048 queries on 10 343 keys of 128 for 8 heads, 4.3e10 flop and 1.7e8 exponentials, take 61 us, 256 on 32 768 31, with the vector unit busy for 53 % of
+// 2048 queries on 10 343 keys of 128 for 8 heads, 4.3e10 flop and 1.7e8 exponentials, take 63 us, 256 on 32 768 31, with the vector unit busy for 53 % of
 // the time and the matrix unit for 34.  Three blocks per compute unit, 1 to 8 parts, and 32 x 32 products with the exponentials spread from step to step
 // took as long (the last at a clock of 2.03 GHz where this has 2.2).
 template <int D, bool F16>
@@ -1061,6 +1065,7 @@ __global__ __launch_bounds__(256) void attend_add_kernel(float* __restrict__ wei
 }
 
 // Parts of the queries in attend_account_kernel: where a row's keys are few blocks, the last turn on the compute units is mostly empty.
+// Though adding up the parts is one more launch: 256 queries on 8 rows of 1000 keys in two parts 39.7 us a call, in one 44.1; 2048 on one row of 4000 in four 57.9 and 111.
 // (No more blocks than 16 turns have: behind those an empty one is little.  It also bounds the sums that the parts leave.)
 constexpr int64_t kPartBlocks = 4096;
 int account_parts(const Keys& k) {
@@ -1077,11 +1082,11 @@ int account_parts(const Keys& k) {
   return best;
 }
 
-constexpr int64_t kMergedKeys = 512;  // of a share (64 rows of up to 4001 keys, 20 queries: 25.2 us, 256 keys 28.8; 8 of 9830, 32 queries, with 64 of 512: 22.9 and 29.8)
+constexpr int64_t kMergedKeys = 512;  // of a share (64 rows of up to 4001 keys, 20 queries: 22.1 us, 256 keys 28.7; 8 of 9830, 32 queries, with 64 of 512: 24.1 and 31.6)
 constexpr int64_t kMostSplits = 512;
 // One launch instead of two (which takes the host 3.5 us less of about 17) where a block per row is not much slower on the device: us, one and two
-// launches, 4 query heads: 4 rows of 256 keys 6.7 and 7.9, 4 of up to 512 8.9 and 8.0, 256 of 512 15.2 and 17.1; but 8 of 1024 12.8 and
-// 8.1, and with more rows than compute units (a block has most of one's LDS) 1024 of 128 27.5 and 19.0.
+// launches, 4 query heads: 4 rows of 256 keys 6.9 and 8.1, 4 of up to 512 9.1 and 8.5 (in a graph, where the host does not count, two would be faster there), 256 of
+// 512 15.7 and 17.5; but 8 of 1024 13.1 and 8.5, and with more rows than compute units (a block has most of one's LDS) 1024 of 128 28.3 and 18.8.
 constexpr int64_t kShortKeys = 512, kShortRows = 256;
 
 Keys keys_of(int64_t rows, int64_t n, int64_t m, int merge, int64_t more, bool account) {
@@ -1192,7 +1197,8 @@ hipError_t launch_attend_of(const AttendArgs& a, void* scratch, hipStream_t stre
     attend_finish_kernel<D, F16, QB, MQ, KP><<<(unsigned)(query_blocks + shared_blocks + own_blocks), 256, 0, stream>>>(a, p, query_blocks, (int)shared_blocks);
   };
   auto finish_of = [&](auto qb) {
-    // Four keys a thread where most compute units still get a block (256 064 of them: 22.4 us a call, one a thread 24.5; 111 408: 24.2 and 23.6).
+    // Four keys a thread where most compute units still get a block (us a call, four and one: 2.1e6 keys of 128, 4 queries 130.0 and 135.3; 256 064, 20 queries,
+    // of 64 22.1 and 22.6, of 128 34.2 and 34.8; 163 840, 32 queries 41.0 and 40.0, 8 queries 22.0 and 21.7; 111 408, 32 queries 25.2 and 24.2).
     auto with = [&](auto mq) {
       if (kept_keys >= 192 * 1024) finish(qb, mq, std::integral_constant<int, 4>{});
       else finish(qb, mq, std::integral_constant<int, 1>{});
