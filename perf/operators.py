@@ -168,7 +168,11 @@ def _attend(s):
     if own:
         from paper_2605_16360_amd import binding as pk
         rows = lambda x: None if x is None else x[0]  # noqa: E731
-        out = pk.proxykv_attend(_ctx(pk), s["q"][0], s["k"][0], s["v"][0], lens=None if c["lens"] == "full" else s["lens"][0], weight=rows(s["weight"]))
+        before = max(c["T"] - c["N"], 0)  # tokens in front of all that the cache has room for: they see nothing, and the call takes no more than it holds
+        q = s["q"][0, :, :, before:].contiguous() if before else s["q"][0]
+        out = pk.proxykv_attend(_ctx(pk), q, s["k"][0], s["v"][0], lens=None if c["lens"] == "full" else s["lens"][0], weight=rows(s["weight"]))
+        if before:
+            out = torch.nn.functional.pad(out, (0, 0, before, 0))
         return {"out": out.unsqueeze(0), "weight": s["weight"]}
     B, H, G, T, D = s["q"].shape
     k, v = s["k"].float(), s["v"].float()
