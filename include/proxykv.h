@@ -241,14 +241,15 @@ int proxykv_compact_pooled(proxykv_ctx* ctx, void* k, void* v, const int32_t* fl
  *   out [rows, group, T, D]
  *   weight [rows, N] fp32  an account of attention, or NULL: see below
  * New token t sees the row's tokens n < lens - T + 1 + t; probabilities are the softmax of <q, k> / sqrt(D) over them, and out their sum
- * of v.  A query that sees nothing (an empty row, more new tokens than the row has, or nothing but logits of -infinity) gets zeros.  Whatever lies in k, v and
- * weight behind a row's tokens is not used, and weight there is left as it was; a token that only some of the T queries see does not touch
- * the others, NaN and infinities in it included.  A value of plus or minus infinity that is seen is that in out, both are a NaN.
+ * of v.  A query that sees nothing (an empty row, more new tokens than the row has, or nothing but logits of -infinity) gets zeros.  Whatever
+ * lies in k, v and weight behind a row's tokens is not used, and weight there is left as it was; a token that only some of the T queries see does
+ * not touch the others, NaN and infinities in it included.  A value of plus or minus infinity that is seen is that in out, both are a NaN.
  * weight[r, n] += the sum of the probabilities that token n gets from the row's group * T queries: over a decode, how much of the
  * attention every cached token has had, by which proxykv_evict selects.  The caller clears it for new tokens.
- * Products of q and k run on MFMA with fp32 accumulation, softmax in fp32; for the product with v a probability is the sum of two values of the
- * cache's type (what rounding leaves of it is at most 2^-16 of it in bf16; in fp16 2^-22, and no less than 2^-36 of the query's largest), for any number of queries. Results do not depend on what else runs: no sum is taken in an order
- * that varies.
+ * Products of q and k run on MFMA with fp32 accumulation, softmax in fp32, for logits of any size that fp32 holds; for the product with v a
+ * probability is the sum of two values of the cache's type, for any number of queries: what rounding leaves of it is at most 2^-16 of it in bf16,
+ * 2^-22 in fp16, and there no less than 2^-36 of the query's largest.  Results do not depend on what else runs: no sum is taken in an order that
+ * varies.
  * D in {64, 128} (PROXYKV_EUNSUPPORTED otherwise), T <= N, rows * group * T < 2^22, rows * N < 2^31; weight and lens may lie on any 4-byte
  * boundary.  out and weight overlap nothing else.
  * While the stream captures, the call allocates nothing, and returns PROXYKV_ESTATE if it takes more workspace than the context has: one call
